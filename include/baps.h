@@ -210,6 +210,27 @@ int baps_attention_fwd_split_noalloc(const void* q, const void* k, const void* v
                                      const baps_params_t* p, void* stream);
 
 /*
+ * Attention with a sliding window and sink tokens: the query row at position
+ * t = r + Sk - Sq (bottom-right aligned) sees key c <= t when c > t - window
+ * or c < sinks.  window >= 1 counts the row's own position; sinks >= 0.  Other
+ * arguments, layouts, empty rows and knobs as baps_attention_fwd_ex (p may be
+ * NULL: canonical knobs), in the E2E HiF8 setup (Alg. 1 over the key blocks
+ * that a row sees; a block that its window hides changes nothing, B0 counts
+ * blocks from key 0, so it holds the sinks) with lambda <= 8 and per-row
+ * restart, or in the Default setup; bf16 Q/K, ties away from zero; else
+ * BAPS_UNSUPPORTED.
+ * workspace: baps_attention_window_workspace(same sizes and knobs) bytes (0
+ * unless rows are few in the Default setup, whose keys are then split over
+ * workgroups), 256-byte aligned, contents undefined on entry and on return;
+ * calls that may overlap need one each.
+ */
+long long baps_attention_window_workspace(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks,
+                                          int block, const baps_params_t* p);
+int baps_attention_window(const void* q, const void* k, const void* v, float* o, float* lse, int B, int Hq, int Hkv,
+                          int Sq, int Sk, int D, int window, int sinks, int block, const baps_params_t* p,
+                          void* workspace, long long workspace_bytes, void* stream);
+
+/*
  * HiF8 codec (the 8-bit format used by every 8-bit step of the method;
  * Sec. 2, App. A).  hif8_encode: codes[i] = code of the HiF8 value nearest
  * to x[i].  flags: BAPS_HIF8_SATURATE clamps finite overflow to +-2^15 (else
@@ -253,6 +274,123 @@ int baps_softmax_block(const float* s, long long rows, long long cols, long long
  * HiF8(2^decode(c)) (App. A, Alg. 2, with exp2 in double precision).
  * Needs no GPU. */
 int baps_get_exp2_lut(unsigned char out_codes[256]);
+
+/*
+ * Paged 8-bit key/value cache.  A pool holds, for every layer, num_pages pages
+ * of `page` tokens of Hkv heads:
+ *   k      [layers][num_pages][Hkv][page][D]        FP8 E4M3 codes
+ *   v      [layers][num_pages][Hkv][page/16][D][16] FP8 E4M3 codes, groups of
+ *                                                   16 tokens transposed
+ *   k_exp, v_exp [layers][num_pages][Hkv]           one scale per page and
+ *          head, as its biased exponent e: a value is code * 2^(e - 127)
+ * The scales are powers of two: a page whose range grows is moved to its new
+ * scale by exact powers of two (plus one 8-bit rounding), as Alg. 1's state
+ * is.  Supported: D in {64, 128}, page in {16, 32, 64, 128}.  The four arrays
+ * are 16-byte aligned device memory of the caller.
+ *
+ * A sequence is a row of a page table, int32 [B][width]: entry j is the page
+ * of tokens [j*page, (j+1)*page).  An entry outside [0, num_pages) is "no
+ * page": its tokens are not written and count as masked keys.  Lengths beyond
+ * width*page (at most 2^30) are taken as width*page.  Tables, lengths, offsets and counts are
+ * device arrays, read when the kernels run (a captured call follows their
+ * contents).  A page may be in several rows; what is appended to goes to pages
+ * that one row holds alone (baps_cache_fork sees to it).
+ */
+typedef struct {
+    unsigned char* k;
+    unsigned char* v;
+    unsigned char* k_exp;
+    unsigned char* v_exp;
+    int layers, num_pages, Hkv, page, D;
+} baps_cache_t;
+
+/*
+ * New tokens into one layer of the cache.  k, v: bf16, element d of head h of
+ * new token t at t*token_stride + h*D + d (token_stride >= Hkv*D, a multiple
+ * of 8; both 16-byte aligned).  Sequence b's new tokens are the packed rows
+ * [cu_new[b], cu_new[b+1]) of the total_new rows, and lens[b] is its length
+ * with them: they become tokens [lens[b] - n, lens[b]).  max_new: at least the
+ * most new tokens of one sequence (tokens past what it announces may stay
+ * unwritten).  A sequence with n <= 0, n > lens[b] or rows outside
+ * [0, total_new] is skipped.
+ * The scale of a page is the least 2^(e-127) >= amax / 448 over its tokens'
+ * |x|, e in [27, 246], and does not fall while the page fills; tokens it held
+ * before are moved to it.  Codes are rounded to nearest, ties to even, +-Inf
+ * and what the scale cannot hold to +-448; NaN stays NaN and sets no scale.
+ * Codes of positions that hold no token stay as they are.
+ */
+int baps_cache_append(const baps_cache_t* cache, int layer, const void* k, const void* v, long long token_stride,
+                      const int* cu_new, const int* lens, const int* table, int table_width, int B, int total_new,
+                      int max_new, void* stream);
+
+/*
+ * Attention over one layer of the cache, eq. (2) with every softmax operation
+ * in fp32 (BAPS_MODE_DEFAULT).  Query rows are packed: sequence b's are
+ * [cu_q[b], cu_q[b+1]) of total_q, the last n of its lens[b] positions; q is
+ * bf16, element d of head h of row t at t*q_stride + h*D + d (q_stride >=
+ * Hq*D, a multiple of 8; 16-byte aligned).  o: bf16 [total_q][Hq][D], 16-byte
+ * aligned; lse: fp32 [total_q][Hq], may be NULL.
+ * The row at position t sees key c when c <= t and, with window > 0, when also
+ * c > t - window or c < sinks.  A row that sees no key gets o = 0 and lse =
+ * -inf.  Rows that belong to no sequence are left as they are.  Keys and
+ * values that no row sees may hold anything; a NaN code or an infinite product
+ * among those that other rows of the call see is not kept from a row whose
+ * own mask hides it.
+ * scale_log2: the score scale in log2 units, 0 for log2(e)/sqrt(D).  max_q and
+ * max_len: at least the most query rows and the longest length of a sequence
+ * (rows past max_q are not computed; max_len only plans the split of the keys).
+ * P enters P V as bf16, with a second bf16 term where rows are few.
+ * workspace: baps_cache_attention_workspace(same sizes) bytes, 256-byte
+ * aligned, contents undefined on entry and on return (NULL when that is 0);
+ * calls that may overlap need one each.
+ */
+long long baps_cache_attention_workspace(const baps_cache_t* cache, int B, int Hq, int total_q, int max_q, int max_len,
+                                         int window, int sinks);
+int baps_cache_attention(const baps_cache_t* cache, int layer, const void* q, long long q_stride, void* o, float* lse,
+                         const int* cu_q, const int* lens, const int* table, int table_width, int B, int Hq,
+                         int total_q, int max_q, int max_len, int window, int sinks, float scale_log2,
+                         void* workspace, long long workspace_bytes, void* stream);
+
+/*
+ * The next set of sequences: child i of B_out goes on from sequence parent[i]
+ * of the B_in old ones (outside [0, B_in): a new, empty sequence).  Forks, drops
+ * (a sequence that no child names), reorders and takes pages for what comes:
+ *   - a child's first ceil(len/page) pages are its parent's, shared; but a
+ *     partly filled last page goes to the parent's first child, if nothing
+ *     else holds it (refs 1), and every other child gets a page of its own
+ *     with a copy of it (all layers, codes and exponents);
+ *   - grow (may be NULL): tokens that child i will append next; it gets the
+ *     pages for them;
+ *   - every page of the old rows loses one reference, every page of the new
+ *     rows has one; pages with none are free, and are taken lowest first, in
+ *     the order of the children (a child's copy first, then what it grows by).
+ *     Pages given back by this call can be taken by it.
+ * refs_in / refs_out [num_pages] int32: references of every page (callers add
+ * their own to hold pages without a row); may be the same array.  table_out
+ * [B_out][width], -1 behind the last page; lens_out [B_out].  Neither may
+ * overlap its input.  *missing (device int32): pages that were wanted and not
+ * found, in the pool or within the table's width; the entries are -1.
+ * workspace: baps_cache_pages_workspace bytes, 256-byte aligned, undefined on
+ * entry and on return.
+ */
+long long baps_cache_pages_workspace(int num_pages, int B_out);
+int baps_cache_fork(const baps_cache_t* cache, const int* table_in, const int* lens_in, const int* refs_in, int B_in,
+                    const int* parent, const int* grow, int B_out, int table_width, int* table_out, int* lens_out,
+                    int* refs_out, int* missing, void* workspace, long long workspace_bytes, void* stream);
+
+/*
+ * Closes the holes of a pool: with n pages in use (refs > 0), the k-th unused
+ * page below n takes the content (all layers) and the references of the k-th
+ * used page from n up.  remap [num_pages]: where each used page went, -1 for
+ * an unused one; table_out = table_in through remap (entries that are no page,
+ * or an unused one, become -1); refs_out is zero from n up; *live = n.
+ * entries: the table's size, rows * width (0 without a table).  table_out may
+ * be table_in and refs_out refs_in.  What a page from n up held is undefined.
+ * workspace as above with B_out = 0.
+ */
+int baps_cache_compact(const baps_cache_t* cache, const int* table_in, long long entries, const int* refs_in,
+                       int* table_out, int* refs_out, int* remap, int* live, void* workspace,
+                       long long workspace_bytes, void* stream);
 
 /* Uploads the score table to the current device (synchronously).  Optional:
  * the first call of an entry point on a device does it otherwise. */

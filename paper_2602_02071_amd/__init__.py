@@ -27,7 +27,10 @@ BAPS_SPLIT_SCRATCH_BYTES = 32 << 20
 EXPORTS = ("baps_attention_fwd", "baps_attention_fwd_ex", "baps_attention_fwd_split", "baps_attention_fwd_dump",
            "baps_attention_fwd_split_noalloc",
            "hif8_encode", "hif8_decode", "baps_softmax_block", "baps_get_exp2_lut", "baps_init",
-           "baps_attention_split_workspace", "baps_last_hip_error", "baps_status_string")
+           "baps_attention_window", "baps_cache_append", "baps_cache_attention", "baps_cache_fork", "baps_cache_compact",
+           "baps_attention_split_workspace", "baps_attention_window_workspace", "baps_cache_attention_workspace",
+           "baps_cache_pages_workspace",
+           "baps_last_hip_error", "baps_status_string")
 
 _lib = None
 
@@ -45,6 +48,12 @@ class baps_params_t(ctypes.Structure):
                 ("b0_last", ctypes.c_int), ("tile_counts", ctypes.c_void_p), ("qk_format", ctypes.c_int),
                 ("q_scale", ctypes.c_float), ("k_scale", ctypes.c_float), ("tie_mode", ctypes.c_int),
                 ("saturate", ctypes.c_int), ("out_bf16", ctypes.c_int)]
+
+
+class baps_cache_t(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("layers", ctypes.c_int), ("num_pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("page", ctypes.c_int),
+                ("D", ctypes.c_int)]
 
 
 # softmax setups (include/baps.h)
@@ -80,6 +89,15 @@ def load():
     L.baps_attention_fwd_split_noalloc.argtypes = [P, P, P, P, P, I, I, I, I, I, I, I, I,
                                                    ctypes.POINTER(baps_params_t), P]
     L.baps_attention_split_workspace.argtypes = [I, I, I, I, I, I, I, ctypes.POINTER(baps_params_t)]
+    L.baps_attention_window.argtypes = [P, P, P, P, P, I, I, I, I, I, I, I, I, I, ctypes.POINTER(baps_params_t), P, LL, P]
+    L.baps_attention_window_workspace.argtypes = [I, I, I, I, I, I, I, I, I, ctypes.POINTER(baps_params_t)]
+    C = ctypes.POINTER(baps_cache_t)
+    L.baps_cache_append.argtypes = [C, I, P, P, LL, P, P, P, I, I, I, I, P]
+    L.baps_cache_attention.argtypes = [C, I, P, LL, P, P, P, P, P, I, I, I, I, I, I, I, I, ctypes.c_float, P, LL, P]
+    L.baps_cache_attention_workspace.argtypes = [C, I, I, I, I, I, I, I]
+    L.baps_cache_fork.argtypes = [C, P, P, P, I, P, P, I, I, P, P, P, P, P, LL, P]
+    L.baps_cache_compact.argtypes = [C, P, LL, P, P, P, P, P, P, LL, P]
+    L.baps_cache_pages_workspace.argtypes = [I, I]
     L.hif8_encode.argtypes = [P, P, LL, I, P]
     L.hif8_decode.argtypes = [P, P, LL, P]
     L.baps_softmax_block.argtypes = [P, LL, LL, LL, I, I, I, I, P, P, P, P, P, P]
@@ -92,6 +110,9 @@ def load():
     for name in EXPORTS[:-2]:
         getattr(L, name).restype = I
     L.baps_attention_split_workspace.restype = LL
+    L.baps_attention_window_workspace.restype = LL
+    L.baps_cache_attention_workspace.restype = LL
+    L.baps_cache_pages_workspace.restype = LL
     _lib = L
     return L
 
@@ -212,6 +233,57 @@ def baps_softmax_block(s, rows, cols, ld_s, block, lam, n_b0, flags, p_codes, re
         _p(d_final), _p(restarted), _stream(stream)))
 
 
+def baps_attention_window_workspace(B, Hq, Hkv, Sq, Sk, D, window, sinks, block, **knobs):
+    """knobs as baps_attention_fwd_ex."""
+    prm = _params(**knobs)
+    return int(load().baps_attention_window_workspace(B, Hq, Hkv, Sq, Sk, D, window, sinks, block, ctypes.byref(prm)))
+
+
+def baps_attention_window(q, k, v, o, lse, B, Hq, Hkv, Sq, Sk, D, window, sinks, block, workspace=None, workspace_bytes=0,
+                          stream=None, **knobs):
+    """knobs as baps_attention_fwd_ex."""
+    prm = _params(**knobs)
+    _check("baps_attention_window", load().baps_attention_window(
+        _p(q), _p(k), _p(v), _p(o), _p(lse), B, Hq, Hkv, Sq, Sk, D, window, sinks, block, ctypes.byref(prm),
+        _p(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def baps_cache_append(cache, layer, k, v, token_stride, cu_new, lens, table, table_width, B, total_new, max_new,
+                      stream=None):
+    _check("baps_cache_append", load().baps_cache_append(
+        ctypes.byref(cache), layer, _p(k), _p(v), token_stride, _p(cu_new), _p(lens), _p(table), table_width, B,
+        total_new, max_new, _stream(stream)))
+
+
+def baps_cache_attention_workspace(cache, B, Hq, total_q, max_q, max_len, window=0, sinks=0):
+    return int(load().baps_cache_attention_workspace(ctypes.byref(cache), B, Hq, total_q, max_q, max_len, window, sinks))
+
+
+def baps_cache_attention(cache, layer, q, q_stride, o, lse, cu_q, lens, table, table_width, B, Hq, total_q, max_q, max_len,
+                         window=0, sinks=0, scale_log2=0.0, workspace=None, workspace_bytes=0, stream=None):
+    _check("baps_cache_attention", load().baps_cache_attention(
+        ctypes.byref(cache), layer, _p(q), q_stride, _p(o), _p(lse), _p(cu_q), _p(lens), _p(table), table_width, B, Hq,
+        total_q, max_q, max_len, window, sinks, scale_log2, _p(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def baps_cache_pages_workspace(num_pages, B_out):
+    return int(load().baps_cache_pages_workspace(num_pages, B_out))
+
+
+def baps_cache_fork(cache, table_in, lens_in, refs_in, B_in, parent, grow, B_out, table_width, table_out, lens_out, refs_out,
+                    missing, workspace, workspace_bytes, stream=None):
+    _check("baps_cache_fork", load().baps_cache_fork(
+        ctypes.byref(cache), _p(table_in), _p(lens_in), _p(refs_in), B_in, _p(parent), _p(grow), B_out, table_width,
+        _p(table_out), _p(lens_out), _p(refs_out), _p(missing), _p(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def baps_cache_compact(cache, table_in, entries, refs_in, table_out, refs_out, remap, live, workspace, workspace_bytes,
+                       stream=None):
+    _check("baps_cache_compact", load().baps_cache_compact(
+        ctypes.byref(cache), _p(table_in), entries, _p(refs_in), _p(table_out), _p(refs_out), _p(remap), _p(live),
+        _p(workspace), int(workspace_bytes), _stream(stream)))
+
+
 def baps_get_exp2_lut():
     buf = (ctypes.c_ubyte * 256)()
     _check("baps_get_exp2_lut", load().baps_get_exp2_lut(buf))
@@ -258,6 +330,26 @@ def attention(q, k, v, causal, block, lse=True, lam=None, n_b0=None, scale_log2=
     return o, l
 
 
+def attention_window(q, k, v, window, sinks=0, block=128, lse=True, stream=None, out_bf16=False, **knobs):
+    """Attention with a sliding window and sink tokens (baps_attention_window):
+    allocates O (and lse) and the workspace with torch.  q [B,Hq,Sq,D], k/v
+    [B,Hkv,Sk,D] bf16 device tensors, contiguous; knobs as
+    baps_attention_fwd_ex (mode, lam, n_b0, scale_log2, b0_last, ...)."""
+    import torch
+    B, Hq, Sq, D = q.shape
+    Hkv, Sk = k.shape[1], k.shape[2]
+    _check_inputs(q, k, v, None)
+    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D or not q.device == k.device == v.device:
+        raise ValueError("k and v must be [B, Hkv, Sk, D] for q [B, Hq, Sq, D], on one device")
+    o = torch.empty((B, Hq, Sq, D), dtype=torch.bfloat16 if out_bf16 else torch.float32, device=q.device)
+    l = torch.empty((B, Hq, Sq), dtype=torch.float32, device=q.device) if lse else None
+    with _on_device(q.device):
+        nbytes = baps_attention_window_workspace(B, Hq, Hkv, Sq, Sk, D, window, sinks, block, **knobs)
+        baps_attention_window(q, k, v, o, l, B, Hq, Hkv, Sq, Sk, D, window, sinks, block,
+                              _scratch(nbytes, q.device, stream), nbytes, stream, out_bf16=out_bf16, **knobs)
+    return o, l
+
+
 def _check_inputs(q, k, v, qk_scales):
     import torch
     qk_dtype = torch.bfloat16 if qk_scales is None else torch.uint8
@@ -295,3 +387,125 @@ def attention_dump(q, k, v, causal, block, rows, lam=1, n_b0=1, scale_log2=0.0, 
                             lam=lam, n_b0=n_b0, scale_log2=scale_log2, mode=mode, restart_rows=restart_rows,
                             b0_last=b0_last, qk_scales=qk_scales, tie_mode=tie_mode, saturate=saturate)
     return o, l, acc[:n, :Sk], ref[:n, :nblk]
+
+
+def _on_device(device):
+    """A guard that makes `device` the current one (none where it is already)."""
+    import contextlib
+    import torch
+    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _scratch(nbytes, device, stream):
+    """A workspace that the caching allocator keeps from others until the call's stream is past it."""
+    import torch
+    if not nbytes:
+        return None
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if stream is not None:
+        ws.record_stream(torch.cuda.ExternalStream(_stream(stream), device=device))
+    return ws
+
+
+class PagedCache:
+    """A paged 8-bit key/value cache over tensors of the caller (include/baps.h
+    states the layout): k [layers, num_pages, Hkv, page, D] and v [layers,
+    num_pages, Hkv, page // 16, D, 16], FP8 E4M3 codes as uint8; k_exp, v_exp
+    [layers, num_pages, Hkv], the scales' exponents as uint8.  Index tensors
+    are int32 on the cache's device; outputs are allocated with torch."""
+
+    def __init__(self, k, v, k_exp, v_exp):
+        import torch
+        if k.dim() != 5:
+            raise ValueError("k must be [layers, num_pages, Hkv, page, D]")
+        layers, pages, Hkv, page, D = k.shape
+        for name, t, shape in (("k", k, k.shape), ("v", v, (layers, pages, Hkv, page // 16, D, 16)),
+                               ("k_exp", k_exp, (layers, pages, Hkv)), ("v_exp", v_exp, (layers, pages, Hkv))):
+            if t.dtype != torch.uint8 or not t.is_contiguous() or not t.is_cuda or t.device != k.device:
+                raise ValueError(f"{name} must be a contiguous uint8 device tensor (all four on one device)")
+            if tuple(t.shape) != tuple(shape):
+                raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+        if D not in (64, 128) or page not in (16, 32, 64, 128):
+            raise ValueError("D must be 64 or 128 and page 16, 32, 64 or 128")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.layers, self.num_pages, self.Hkv, self.page, self.D = layers, pages, Hkv, page, D
+        self.device = k.device
+        self.c = baps_cache_t(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), layers, pages, Hkv, page, D)
+
+    @classmethod
+    def zeros(cls, layers, num_pages, Hkv, page, D, device="cuda"):
+        import torch
+        z = lambda *s: torch.zeros(s, dtype=torch.uint8, device=device)  # noqa: E731
+        return cls(z(layers, num_pages, Hkv, page, D), z(layers, num_pages, Hkv, page // 16, D, 16),
+                   z(layers, num_pages, Hkv), z(layers, num_pages, Hkv))
+
+    def _ints(self, **tensors):
+        import torch
+        for name, (t, dim, n) in tensors.items():
+            if t.dtype != torch.int32 or not t.is_contiguous() or t.device != self.device or t.dim() != dim:
+                raise ValueError(f"{name} must be a contiguous int32 tensor of {dim} dimension(s) on {self.device}")
+            if n is not None and t.shape[0] != n:
+                raise ValueError(f"{name} must have {n} rows, not {t.shape[0]}")
+
+    def _rows(self, name, t, heads):
+        """Packed bf16 rows [T, heads, D], the heads of a row next to each other; returns the row stride."""
+        import torch
+        if (t.dtype != torch.bfloat16 or t.device != self.device or t.dim() != 3 or tuple(t.shape[1:]) != (heads, self.D)
+                or t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.D)):
+            raise ValueError(f"{name} must be bf16 [T, {heads}, {self.D}] on {self.device} with contiguous rows")
+        return t.stride(0) if t.shape[0] > 1 else heads * self.D
+
+    def append(self, layer, k, v, cu_new, lens, table, max_new, stream=None):
+        """k, v [T, Hkv, D] bf16: the new tokens of every sequence, packed (rows may be strided, both alike)."""
+        B = lens.shape[0]
+        self._ints(cu_new=(cu_new, 1, B + 1), lens=(lens, 1, B), table=(table, 2, B))
+        stride = self._rows("k", k, self.Hkv)
+        if self._rows("v", v, self.Hkv) != stride or k.shape[0] != v.shape[0]:
+            raise ValueError("k and v must have the same rows and row stride")
+        with _on_device(self.device):
+            baps_cache_append(self.c, layer, k, v, stride, cu_new, lens, table, table.shape[1], B, k.shape[0], max_new,
+                              stream)
+
+    def attention(self, layer, q, cu_q, lens, table, max_q, max_len, window=0, sinks=0, scale_log2=0.0, lse=True,
+                  stream=None):
+        """q [T, Hq, D] bf16, packed (rows may be strided); returns o [T, Hq, D] bf16 and lse [T, Hq] (or None)."""
+        import torch
+        B = lens.shape[0]
+        self._ints(cu_q=(cu_q, 1, B + 1), lens=(lens, 1, B), table=(table, 2, B))
+        T, Hq = q.shape[0], q.shape[1]
+        stride = self._rows("q", q, Hq)
+        o = torch.empty((T, Hq, self.D), dtype=torch.bfloat16, device=self.device)
+        l = torch.empty((T, Hq), dtype=torch.float32, device=self.device) if lse else None
+        with _on_device(self.device):
+            nbytes = baps_cache_attention_workspace(self.c, B, Hq, T, max_q, max_len, window, sinks)
+            baps_cache_attention(self.c, layer, q, stride, o, l, cu_q, lens, table, table.shape[1], B, Hq, T, max_q,
+                                 max_len, window, sinks, scale_log2, _scratch(nbytes, self.device, stream), nbytes, stream)
+        return o, l
+
+    def fork(self, table, lens, refs, parent, grow=None, stream=None):
+        """The next set of sequences: (table, lens, refs, missing), new tensors; the pool's copies are made in place."""
+        import torch
+        B_in, width = table.shape
+        B_out = parent.shape[0]
+        self._ints(table=(table, 2, B_in), lens=(lens, 1, B_in), refs=(refs, 1, self.num_pages), parent=(parent, 1, B_out))
+        if grow is not None:
+            self._ints(grow=(grow, 1, B_out))
+        new = lambda *s: torch.empty(s, dtype=torch.int32, device=self.device)  # noqa: E731
+        out, lens_out, refs_out, missing = new(B_out, width), new(B_out), new(self.num_pages), new(1)
+        with _on_device(self.device):
+            nbytes = baps_cache_pages_workspace(0, B_out)
+            baps_cache_fork(self.c, table, lens, refs, B_in, parent, grow, B_out, width, out, lens_out, refs_out, missing,
+                            _scratch(nbytes, self.device, stream), nbytes, stream)
+        return out, lens_out, refs_out, missing
+
+    def compact(self, table, refs, stream=None):
+        """(table, refs, remap, live), new tensors; the pool's pages are moved in place."""
+        import torch
+        self._ints(table=(table, 2, None), refs=(refs, 1, self.num_pages))
+        out, refs_out, remap = torch.empty_like(table), torch.empty_like(refs), torch.empty_like(refs)
+        live = torch.empty(1, dtype=torch.int32, device=self.device)
+        with _on_device(self.device):
+            nbytes = baps_cache_pages_workspace(self.num_pages, 0)
+            baps_cache_compact(self.c, table, table.numel(), refs, out, refs_out, remap, live,
+                               _scratch(nbytes, self.device, stream), nbytes, stream)
+        return out, refs_out, remap, live

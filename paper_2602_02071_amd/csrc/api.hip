@@ -5,6 +5,7 @@
 #include <mutex>
 
 #include "../../include/baps.h"
+#include "cache.hpp"
 #include "common.hpp"
 
 namespace {
@@ -322,6 +323,9 @@ int make_params(const void* q, const void* k, const void* v, float* o, float* ls
     p.dump_acc = nullptr;
     p.dump_ref = nullptr;
     p.dump_nblk = 0;
+    p.window = p.sinks = 0;
+    p.nsplit = 1;
+    p.part = p.ml = nullptr;
     // the score scale in log2 units; with FP8 Q/K the dequantisation scales
     // fold into it, in double, rounded once
     const double base = kn.scale_log2 > 0.0f ? (double)kn.scale_log2 : 1.4426950408889634 / std::sqrt((double)D);
@@ -430,6 +434,92 @@ int split_impl(const void* q, const void* k, const void* v, float* o, float* lse
     sp.bps = plan.bps;
     clear_stale_error();
     return status_of(launch_attention_split(sp, D, block, static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------- windows
+// The splits of a windowed call with few rows (Default setup) and their
+// workspace: about two workgroups per CU, of two key blocks at least each.
+void window_plan(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks, int block, int mode, int* nsplit,
+                 long long* bytes)
+{
+    *nsplit = 1;
+    *bytes = 0;
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv || block <= 0 || mode != BAPS_MODE_DEFAULT) return;
+    const long long flat = (long long)Sq * (Hq / Hkv);
+    if (flat > kFewFlatRows) return;
+    int ncu = 256;                                  // (without a device: an MI355X)
+    if (cu_count(&ncu) != hipSuccess) {
+        clear_stale_error();
+        ncu = 256;
+    }
+    long long keys = (long long)window + sinks + Sq + 2 * block;
+    if (keys > Sk) keys = Sk;
+    long long n = 2LL * ncu / ((flat + 15) / 16 * Hkv * B);
+    const long long most = (keys + block - 1) / block / 2;
+    if (n > most) n = most;
+    *nsplit = (int)(n < 1 ? 1 : (n > 64 ? 64 : n));
+    if (*nsplit > 1) *bytes = align256(*nsplit * (long long)B * Hq * Sq * (D + 2) * 4);
+}
+
+// ---------------------------------------------------------------- the cache
+bool cache_ok(const baps_cache_t* c)
+{
+    return c && c->layers >= 0 && c->num_pages >= 0 && c->Hkv >= 0 && c->page >= 0 && c->D >= 0;
+}
+
+bool cache_supported(const baps_cache_t& c)
+{
+    return (c.D == 64 || c.D == 128) && (c.page == 16 || c.page == 32 || c.page == 64 || c.page == 128) && c.Hkv <= 32767;
+}
+
+bool cache_arrays(const baps_cache_t& c)
+{
+    return c.k && c.v && c.k_exp && c.v_exp && aligned16(c.k) && aligned16(c.v);
+}
+
+CacheView cache_layer(const baps_cache_t& c, int layer)
+{
+    const long long heads = (long long)layer * c.num_pages * c.Hkv, bytes = (long long)c.page * c.D;
+    CacheView v;
+    v.k = c.k + heads * bytes;
+    v.v = c.v + heads * bytes;
+    v.ke = c.k_exp + heads;
+    v.ve = c.v_exp + heads;
+    v.num_pages = c.num_pages;
+    v.Hkv = c.Hkv;
+    v.lpage = c.page == 16 ? 4 : (c.page == 32 ? 5 : (c.page == 64 ? 6 : 7));
+    return v;
+}
+
+// Tokens that a table row can name fit an int with room to spare
+bool width_ok(const baps_cache_t& c, int table_width) { return (long long)table_width * c.page <= (1LL << 30); }
+
+// The splits of a cache attention call and their workspace
+int cache_plan(const baps_cache_t& c, int B, int Hq, int total_q, int max_q, int max_len, int window, int sinks,
+               int* nsplit, long long* bytes)
+{
+    *nsplit = 1;
+    *bytes = 0;
+    if (B <= 0 || Hq <= 0 || c.Hkv <= 0 || Hq % c.Hkv || max_q <= 0 || max_len <= 0 || total_q <= 0) return BAPS_OK;
+    int ncu = 256;                                  // (without a device: an MI355X)
+    if (cu_count(&ncu) != hipSuccess) {
+        clear_stale_error();
+        ncu = 256;
+    }
+    *nsplit = cache_attention_splits(B, Hq, c.Hkv, max_q, max_len, window, sinks, ncu);
+    if (*nsplit > 1) *bytes = align256((long long)*nsplit * total_q * Hq * (c.D + 2) * 4);
+    return BAPS_OK;
+}
+
+bool workspace_ok(const void* workspace, long long have, long long need)
+{
+    return need == 0 || (workspace && have >= need && !((uintptr_t)workspace & 255u));
+}
+
+bool overlap(const void* a, const void* b, long long bytes_a, long long bytes_b)
+{
+    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+    return bytes_a > 0 && bytes_b > 0 && x < y + bytes_b && y < x + bytes_a;
 }
 
 }  // namespace
@@ -558,6 +648,200 @@ int baps_softmax_block(const float* s, long long rows, long long cols, long long
         p.restarted = restarted; p.tab = tab;
         clear_stale_error();
         return status_of(launch_softmax_block(p, static_cast<hipStream_t>(stream)));
+    } catch (...) {
+        return BAPS_HIP_ERROR;
+    }
+}
+
+long long baps_attention_window_workspace(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks, int block,
+                                          const baps_params_t* prm)
+{
+    if (window < 1 || sinks < 0) return 0;
+    int nsplit = 1;
+    long long bytes = 0;
+    window_plan(B, Hq, Hkv, Sq, Sk, D, window, sinks, block, knobs_of(prm).mode, &nsplit, &bytes);
+    return bytes;
+}
+
+int baps_attention_window(const void* q, const void* k, const void* v, float* o, float* lse, int B, int Hq, int Hkv,
+                          int Sq, int Sk, int D, int window, int sinks, int block, const baps_params_t* prm,
+                          void* workspace, long long workspace_bytes, void* stream)
+{
+    if (window < 1 || sinks < 0) return BAPS_INVALID_ARGUMENT;
+    try {
+        const baps_params_t kn = knobs_of(prm);
+        AttnParams p;
+        bool empty = false;
+        int st = make_params(q, k, v, o, lse, B, Hq, Hkv, Sq, Sk, D, 1, block, kn, &p, &empty);
+        if (st || empty) return st;
+        if (kn.mode == BAPS_MODE_EXP2_HIF8 || (kn.mode == BAPS_MODE_E2E_HIF8 && kn.lambda > kCodeMaxLambda) || p.qk_f8 ||
+            p.tie_even || p.restart_rows > 1)
+            return BAPS_UNSUPPORTED;
+        long long bytes = 0;
+        window_plan(B, Hq, Hkv, Sq, Sk, D, window, sinks, block, kn.mode, &p.nsplit, &bytes);
+        if (!workspace_ok(workspace, workspace_bytes, bytes)) return BAPS_INVALID_ARGUMENT;
+        if ((st = attach_tables(&p))) return st;
+        // a window or a sink past the keys is all of them (and sums stay in range)
+        p.window = window < Sk ? window : (Sk > 0 ? Sk : 1);
+        p.sinks = sinks < Sk ? sinks : Sk;
+        p.part = static_cast<float*>(workspace);
+        p.ml = p.part + (long long)p.nsplit * B * Hq * Sq * D;
+        clear_stale_error();
+        return status_of(launch_attention_window(p, D, block, static_cast<hipStream_t>(stream)));
+    } catch (...) {
+        return BAPS_HIP_ERROR;
+    }
+}
+
+int baps_cache_append(const baps_cache_t* cache, int layer, const void* k, const void* v, long long token_stride,
+                      const int* cu_new, const int* lens, const int* table, int table_width, int B, int total_new,
+                      int max_new, void* stream)
+{
+    if (!cache_ok(cache) || B < 0 || total_new < 0 || max_new < 0 || table_width < 0) return BAPS_INVALID_ARGUMENT;
+    if (layer < 0 || layer >= cache->layers) return BAPS_INVALID_ARGUMENT;
+    if (B == 0 || total_new == 0 || max_new == 0 || cache->Hkv == 0 || cache->num_pages == 0 || table_width == 0)
+        return BAPS_OK;
+    if (!cache_supported(*cache) || !width_ok(*cache, table_width)) return BAPS_UNSUPPORTED;
+    if (!cache_arrays(*cache) || !k || !v || !cu_new || !lens || !table) return BAPS_INVALID_ARGUMENT;
+    if (!aligned16(k) || !aligned16(v) || token_stride < (long long)cache->Hkv * cache->D || token_stride % 8)
+        return BAPS_INVALID_ARGUMENT;
+    if (((long long)max_new + 2 * cache->page - 2) / cache->page * B > 0x7fffffffLL) return BAPS_UNSUPPORTED;
+    try {
+        CacheAppendParams p;
+        p.c = cache_layer(*cache, layer);
+        p.k = static_cast<const uint16_t*>(k);
+        p.v = static_cast<const uint16_t*>(v);
+        p.stride = token_stride;
+        p.cu = cu_new; p.lens = lens; p.table = table;
+        p.table_width = table_width; p.B = B; p.max_new = max_new; p.total = total_new;
+        clear_stale_error();
+        return status_of(launch_cache_append(p, cache->D, static_cast<hipStream_t>(stream)));
+    } catch (...) {
+        return BAPS_HIP_ERROR;
+    }
+}
+
+long long baps_cache_attention_workspace(const baps_cache_t* cache, int B, int Hq, int total_q, int max_q, int max_len,
+                                         int window, int sinks)
+{
+    if (!cache_ok(cache) || !cache_supported(*cache) || window < 0 || sinks < 0) return 0;
+    int nsplit = 1;
+    long long bytes = 0;
+    cache_plan(*cache, B, Hq, total_q, max_q, max_len, window, sinks, &nsplit, &bytes);
+    return bytes;
+}
+
+int baps_cache_attention(const baps_cache_t* cache, int layer, const void* q, long long q_stride, void* o, float* lse,
+                         const int* cu_q, const int* lens, const int* table, int table_width, int B, int Hq,
+                         int total_q, int max_q, int max_len, int window, int sinks, float scale_log2,
+                         void* workspace, long long workspace_bytes, void* stream)
+{
+    if (!cache_ok(cache) || B < 0 || Hq < 0 || total_q < 0 || max_q < 0 || max_len < 0 || table_width < 0 || window < 0 ||
+        sinks < 0 || !(scale_log2 >= 0.0f) || std::isinf(scale_log2))
+        return BAPS_INVALID_ARGUMENT;
+    if (layer < 0 || layer >= cache->layers) return BAPS_INVALID_ARGUMENT;
+    if (B == 0 || Hq == 0 || total_q == 0 || max_q == 0) return BAPS_OK;
+    if (cache->Hkv == 0 || Hq % cache->Hkv) return BAPS_INVALID_ARGUMENT;
+    if (!cache_supported(*cache) || !width_ok(*cache, table_width) || B > 65535 || cache->num_pages == 0 || table_width == 0)
+        return BAPS_UNSUPPORTED;
+    if ((long long)max_q * (Hq / cache->Hkv) > (1LL << 30) || 4LL * cache->Hkv > 65535) return BAPS_UNSUPPORTED;
+    if (!cache_arrays(*cache) || !q || !o || !cu_q || !lens || !table) return BAPS_INVALID_ARGUMENT;
+    if (!aligned16(q) || !aligned16(o) || q_stride < (long long)Hq * cache->D || q_stride % 8) return BAPS_INVALID_ARGUMENT;
+    try {
+        CacheAttnParams p;
+        long long bytes = 0;
+        if (int st = cache_plan(*cache, B, Hq, total_q, max_q, max_len, window, sinks, &p.nsplit, &bytes)) return st;
+        if (!workspace_ok(workspace, workspace_bytes, bytes)) return BAPS_INVALID_ARGUMENT;
+        p.c = cache_layer(*cache, layer);
+        p.q = static_cast<const uint16_t*>(q);
+        p.qstride = q_stride;
+        p.o = static_cast<uint16_t*>(o);
+        p.lse = lse;
+        p.cu = cu_q; p.lens = lens; p.table = table;
+        p.table_width = table_width; p.B = B; p.Hq = Hq; p.total_q = total_q; p.max_q = max_q;
+        p.window = window; p.sinks = sinks;
+        p.scale = scale_log2 > 0.0f ? scale_log2 : (float)(1.4426950408889634 / std::sqrt((double)cache->D));
+        p.part = static_cast<float*>(workspace);
+        p.ml = p.part + (long long)p.nsplit * total_q * Hq * cache->D;
+        clear_stale_error();
+        return status_of(launch_cache_attention(p, cache->D, static_cast<hipStream_t>(stream)));
+    } catch (...) {
+        return BAPS_HIP_ERROR;
+    }
+}
+
+long long baps_cache_pages_workspace(int num_pages, int B_out)
+{
+    if (num_pages < 0 || B_out < 0) return 0;
+    const long long fork = 5LL * B_out + 1, compact = 3LL * num_pages + 1;
+    return align256(4 * (fork > compact ? fork : compact));
+}
+
+int baps_cache_fork(const baps_cache_t* cache, const int* table_in, const int* lens_in, const int* refs_in, int B_in,
+                    const int* parent, const int* grow, int B_out, int table_width, int* table_out, int* lens_out,
+                    int* refs_out, int* missing, void* workspace, long long workspace_bytes, void* stream)
+{
+    if (!cache_ok(cache) || B_in < 0 || B_out < 0 || table_width < 0) return BAPS_INVALID_ARGUMENT;
+    if (!cache_supported(*cache) || !width_ok(*cache, table_width)) return BAPS_UNSUPPORTED;
+    if (cache->layers > 65535 || (long long)B_in + B_out > 0x7fffffffLL ||
+        (long long)B_out * table_width > 0x7fffffffLL)
+        return BAPS_UNSUPPORTED;
+    const bool rows_in = B_in > 0 && table_width > 0, rows_out = B_out > 0 && table_width > 0;
+    if (!missing || (cache->num_pages > 0 && (!refs_in || !refs_out)) || (rows_in && !table_in) || (B_in > 0 && !lens_in) ||
+        (B_out > 0 && (!parent || !lens_out)) || (rows_out && !table_out))
+        return BAPS_INVALID_ARGUMENT;
+    if (cache->layers > 0 && cache->num_pages > 0 && cache->Hkv > 0 && !cache_arrays(*cache)) return BAPS_INVALID_ARGUMENT;
+    const long long tin = 4LL * B_in * table_width, tout = 4LL * B_out * table_width;
+    if (overlap(table_in, table_out, tin, tout) || overlap(lens_in, lens_out, 4LL * B_in, 4LL * B_out) ||
+        (refs_in != refs_out && overlap(refs_in, refs_out, 4LL * cache->num_pages, 4LL * cache->num_pages)))
+        return BAPS_INVALID_ARGUMENT;
+    if (!workspace_ok(workspace, workspace_bytes, baps_cache_pages_workspace(0, B_out))) return BAPS_INVALID_ARGUMENT;
+    try {
+        CacheForkParams p;
+        p.k = cache->k; p.v = cache->v; p.ke = cache->k_exp; p.ve = cache->v_exp;
+        p.layers = cache->layers; p.num_pages = cache->num_pages; p.Hkv = cache->Hkv; p.page = cache->page; p.D = cache->D;
+        p.table_in = table_in; p.lens_in = lens_in; p.refs_in = refs_in; p.parent = parent; p.grow = grow;
+        p.table_out = table_out; p.lens_out = lens_out; p.refs_out = refs_out; p.missing = missing;
+        p.B_in = B_in; p.B_out = B_out; p.width = table_width;
+        p.src = static_cast<int*>(workspace);
+        p.dst = p.src + B_out;
+        p.taken = p.dst + B_out;
+        p.over = p.taken + B_out;
+        p.fresh = p.over + B_out;
+        clear_stale_error();
+        return status_of(launch_cache_fork(p, static_cast<hipStream_t>(stream)));
+    } catch (...) {
+        return BAPS_HIP_ERROR;
+    }
+}
+
+int baps_cache_compact(const baps_cache_t* cache, const int* table_in, long long entries, const int* refs_in,
+                       int* table_out, int* refs_out, int* remap, int* live, void* workspace,
+                       long long workspace_bytes, void* stream)
+{
+    if (!cache_ok(cache) || entries < 0) return BAPS_INVALID_ARGUMENT;
+    if (!cache_supported(*cache)) return BAPS_UNSUPPORTED;
+    if (!live || (cache->num_pages > 0 && (!refs_in || !refs_out || !remap)) || (entries > 0 && (!table_in || !table_out)))
+        return BAPS_INVALID_ARGUMENT;
+    if (cache->layers > 0 && cache->num_pages > 0 && cache->Hkv > 0 && !cache_arrays(*cache)) return BAPS_INVALID_ARGUMENT;
+    if ((table_in != table_out && overlap(table_in, table_out, 4 * entries, 4 * entries)) ||
+        (refs_in != refs_out && overlap(refs_in, refs_out, 4LL * cache->num_pages, 4LL * cache->num_pages)))
+        return BAPS_INVALID_ARGUMENT;
+    if (!workspace_ok(workspace, workspace_bytes, baps_cache_pages_workspace(cache->num_pages, 0)))
+        return BAPS_INVALID_ARGUMENT;
+    try {
+        CacheCompactParams p;
+        p.k = cache->k; p.v = cache->v; p.ke = cache->k_exp; p.ve = cache->v_exp;
+        p.layers = cache->layers; p.num_pages = cache->num_pages; p.Hkv = cache->Hkv; p.page = cache->page; p.D = cache->D;
+        p.refs_in = refs_in; p.table_in = table_in;
+        p.refs_out = refs_out; p.table_out = table_out; p.remap = remap; p.live = live;
+        p.entries = entries;
+        p.moves = static_cast<int*>(workspace);
+        p.from = p.moves + 1;
+        p.to = p.from + cache->num_pages;
+        p.held = p.to + cache->num_pages;
+        clear_stale_error();
+        return status_of(launch_cache_compact(p, static_cast<hipStream_t>(stream)));
     } catch (...) {
         return BAPS_HIP_ERROR;
     }

@@ -86,9 +86,17 @@ __device__ __forceinline__ void wait_vm(int n)
 // TIE: the 8-bit cast of T rounds ties to even (a second code table covers
 // the T whose bits 18..0 are zero).  DUMP: also write the raw dot products and
 // block references of the rows the caller marks (AttnParams::dump_slot).
-template <int D, int BLK, bool CT, int MODE, bool F8, bool TIE, bool DUMP>
+// MODE_: the softmax setup, with kModeWindow for a windowed call.  Its workgroup
+// takes one of nsplit equal parts of the blocks that its rows reach (more than
+// one in the Default setup only); a part's sums go to part and ml, and
+// baps_attn_window_combine_kernel joins them.
+template <int D, int BLK, bool CT, int MODE_, bool F8, bool TIE, bool DUMP>
 __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnParams p)
 {
+    constexpr int MODE = MODE_ & ~kModeWindow;
+    constexpr bool WIN = (MODE_ & kModeWindow) != 0;
+    constexpr bool kParts = WIN && MODE == kModeDefault;   // keys split over workgroups, P in two bf16 terms
+    static_assert(!WIN || (CT && !F8 && !TIE && !DUMP), "windowed calls: bf16 Q/K");
     static_assert(MODE == kModeE2E || CT, "the eq. (2) setups use the compact table (T <= 0)");
     static_assert(!TIE || (MODE == kModeE2E && CT && !F8), "ties to even: canonical path");
     static_assert(D == 64 || D == 128, "head dimension");
@@ -116,7 +124,7 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
 
     const int G = p.Hq / p.Hkv;
     const int flat_rows = p.Sq * G;
-    const int tile = blockIdx.x;
+    const int tile = kParts ? blockIdx.x / p.nsplit : blockIdx.x;
     const int g = blockIdx.y;
     const int b = blockIdx.z;
     const uint16_t* kbase = p.k + ((long long)b * p.Hkv + g) * (long long)p.Sk * D;
@@ -127,14 +135,27 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
     const int off = p.Sk - p.Sq;
     const int f_last = min(flat_rows - 1, tile * kRows + kRows - 1);
     const int kmax_tile = p.causal ? min(p.Sk - 1, f_last / G + off) : p.Sk - 1;
-    const int nblk = kmax_tile < 0 ? 0 : kmax_tile / BLK + 1;
+    KeyBlocks kb = {};
+    int jx0 = 0, nblk;                            // this workgroup's blocks: [jx0, jx0 + nblk) of the list
+    if constexpr (WIN) {
+        kb = key_blocks<BLK>(tile * kRows / G + off, kmax_tile, p.window, p.sinks);
+        nblk = kb.n;
+        if constexpr (kParts) {
+            const int per = (kb.n + p.nsplit - 1) / p.nsplit;
+            jx0 = blockIdx.x % p.nsplit * per;
+            nblk = max(0, min(per, kb.n - jx0));
+        }
+    } else {
+        nblk = kmax_tile < 0 ? 0 : kmax_tile / BLK + 1;
+    }
+    auto block_of = [&](int jx) { return WIN ? kb.block(jx0 + jx) : jx; };
     const int nslots = 2 * nblk;                  // this wave's slots: K then V of each block
 
     // slot n of this wave: block n/2, keys 32*wave .. +32 of the block; K if n is even
     const uint32_t my_ring_lds = ring_lds + (uint32_t)(wave * RW * C::kSlotBytes);
     const char* my_ring = ring + wave * RW * C::kSlotBytes;
     auto issue_slot = [&](int n) {
-        const int jb = n >> 1;
+        const int jb = block_of(n >> 1);
         const bool is_v = (n & 1) != 0;
         const int key0 = jb * BLK + wave * kSlotKeys;
         const uint32_t dst = my_ring_lds + (uint32_t)((n % RW) * C::kSlotBytes);
@@ -195,6 +216,13 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) kmax_lo = min(kmax_lo, __shfl_xor(kmax_lo, o, 64));
     kmax_lo = __builtin_amdgcn_readfirstlane(kmax_lo);
+    const int kmin = (WIN && row_ok) ? max(0, r + off - p.window + 1) : 0;       // sinks apart
+    int kmin_hi = kmin;
+    if constexpr (WIN) {
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) kmin_hi = max(kmin_hi, __shfl_xor(kmin_hi, o, 64));
+        kmin_hi = __builtin_amdgcn_readfirstlane(kmin_hi);
+    }
 
     // Q^T as the B operand of S^T = K Q^T (16x16x32): lane holds
     // Q[row][32*kk + 8*grp .. +8]; K uses the same d order
@@ -249,7 +277,8 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
     __syncthreads();                              // code table published
 
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-    for (int jb = 0; jb < nblk; ++jb) {
+    for (int jx = 0; jx < nblk; ++jx) {
+        const int jb = block_of(jx);
         const int key0 = jb * BLK + wave * kSlotKeys;   // this wave's first key of the block
         // S^T = K Q^T for this wave's 32 keys: two 16-key tiles
         f32x4 sacc[2];
@@ -294,6 +323,14 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
                 for (int i = 0; i < 4; ++i)
                     if (16 * t2 + i > lim) sacc[t2][i] = ninf;
         }
+        if (WIN && key0 < kmin_hi && key0 + kSlotKeys > p.sinks) {
+            const int lim = kmin - key0 - 4 * grp, snk = p.sinks - key0 - 4 * grp;
+#pragma unroll
+            for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sacc[t2][i] = (16 * t2 + i < lim) & (16 * t2 + i >= snk) ? ninf : sacc[t2][i];
+        }
         if constexpr (DUMP) {
             if (dslot >= 0) {
                 float* dst = p.dump_acc + (long long)dslot * p.Sk;
@@ -314,11 +351,11 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
         pm = __builtin_fmaxf(pm, __shfl_xor(pm, 32, 64));
         float amax = pm;
         if constexpr (KW > 1) {
-            if (grp == 0) xch[jb & 1][wave][c16] = pm;
+            if (grp == 0) xch[jx & 1][wave][c16] = pm;
             __syncthreads();
-            amax = xch[jb & 1][0][c16];
+            amax = xch[jx & 1][0][c16];
 #pragma unroll
-            for (int w = 1; w < KW; ++w) amax = __builtin_fmaxf(amax, xch[jb & 1][w][c16]);
+            for (int w = 1; w < KW; ++w) amax = __builtin_fmaxf(amax, xch[jx & 1][w][c16]);
         }
 
         float nref;
@@ -388,7 +425,7 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
 
         // P = HiF8(2^HiF8(T)) of the 32 keys as one B operand: slots 0..3 =
         // keys 4*grp + i, slots 4..7 = keys 16 + 4*grp + i
-        u32x4 pop;
+        u32x4 pop, pop_lo = {};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int t2 = e >> 1;
@@ -398,6 +435,11 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
                 const float p1 = __builtin_amdgcn_exp2f(sacc[t2][2 * (e & 1) + 1] * c + nref);
                 const bf16x2 pb = {(__bf16)p0, (__bf16)p1};
                 pop[e] = __builtin_bit_cast(uint32_t, pb);
+                if constexpr (kParts) {
+                    // the second term: P = hi + lo to 2^-17 (the keys' bytes bound this kernel)
+                    const bf16x2 pl = {(__bf16)(p0 - (float)pb[0]), (__bf16)(p1 - (float)pb[1])};
+                    pop_lo[e] = __builtin_bit_cast(uint32_t, pl);
+                }
                 dl += p0 + p1;
                 continue;
             }
@@ -435,6 +477,8 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
                 const u32x4 a = {__builtin_bit_cast(u32x2, va)[0], __builtin_bit_cast(u32x2, va)[1],
                                  __builtin_bit_cast(u32x2, vb)[0], __builtin_bit_cast(u32x2, vb)[1]};
                 oacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(pop), oacc[t], 0, 0, 0);
+                if constexpr (kParts)
+                    oacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(pop_lo), oacc[t], 0, 0, 0);
             }
             next_slot();
         }
@@ -471,6 +515,18 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
     }
     if (!row_ok) return;
     const long long orow_off = (((long long)b * p.Hq + h) * p.Sq + r) * D;
+    if constexpr (kParts) {
+        if (p.nsplit > 1) {
+            const long long at = blockIdx.x % p.nsplit * ((long long)p.B * p.Hq * p.Sq) + orow_off / D;
+#pragma unroll
+            for (int t = 0; t < kDT; ++t) *reinterpret_cast<f32x4*>(p.part + at * D + 16 * t + 4 * grp) = oacc[t];
+            if (grp == 0) {
+                p.ml[2 * at] = ref;
+                p.ml[2 * at + 1] = dw;
+            }
+            return;
+        }
+    }
     const bool empty = (ref == ninf);
     const float inv = empty ? 0.0f : 1.0f / dw;
     if (p.out_bf16) {
@@ -527,7 +583,8 @@ hipError_t launch_dec(const AttnParams& p, hipStream_t st)
         attr_set.mark(dev);
     }
     const long long flat = (long long)p.Sq * (p.Hq / p.Hkv);
-    const dim3 grid((unsigned)((flat + kRows - 1) / kRows), (unsigned)p.Hkv, (unsigned)p.B);
+    const int parts = MODE == (kModeDefault | kModeWindow) ? p.nsplit : 1;
+    const dim3 grid((unsigned)((flat + kRows - 1) / kRows * parts), (unsigned)p.Hkv, (unsigned)p.B);
     hipLaunchKernelGGL((baps_attn_decode_kernel<D, BLK, CT, MODE, F8, TIE, DUMP>), grid, dim3(64 * C::kWaves),
                        C::kLdsBytes, st, p);
     return hipGetLastError();
@@ -565,6 +622,69 @@ hipError_t launch_attention_decode(const AttnParams& p, int D, int block, hipStr
     if (D == 128 && block == 32) return launch_dec_any<128, 32>(p, st);
     if (D == 128 && block == 64) return launch_dec_any<128, 64>(p, st);
     if (D == 128 && block == 128) return launch_dec_any<128, 128>(p, st);
+    return hipErrorInvalidValue;
+}
+
+namespace {
+
+// Joins a row's parts: their common maximum, then the weighted sums in the
+// parts' order.  One row per D/4 lanes.
+template <int D>
+__global__ __launch_bounds__(256) void baps_attn_window_combine_kernel(AttnParams p)
+{
+    constexpr int kLanes = D / 4, kPer = 256 / kLanes;
+    const long long rows = (long long)p.B * p.Hq * p.Sq;
+    const long long row = (long long)blockIdx.x * kPer + threadIdx.x / kLanes;
+    const int d = threadIdx.x % kLanes * 4;
+    if (row >= rows) return;
+    const float ninf = -__builtin_huge_valf();
+    float m = ninf, l = 0.0f;
+    for (int k = 0; k < p.nsplit; ++k) m = __builtin_fmaxf(m, p.ml[2 * (k * rows + row)]);
+    f32x4 o = {};
+    for (int k = 0; k < p.nsplit; ++k) {
+        const float mk = p.ml[2 * (k * rows + row)];
+        if (mk == ninf) continue;
+        const float w = __builtin_amdgcn_exp2f(mk - m);
+        l += w * p.ml[2 * (k * rows + row) + 1];
+        const f32x4 x = *reinterpret_cast<const f32x4*>(p.part + (k * rows + row) * D + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += w * x[e];
+    }
+    const bool empty = m == ninf;
+    const float inv = empty ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= inv;
+    if (p.out_bf16) {
+        const bf16x2 lo = {(__bf16)o[0], (__bf16)o[1]}, hi = {(__bf16)o[2], (__bf16)o[3]};
+        *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(p.o) + row * D + d) =
+            u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+    } else {
+        *reinterpret_cast<f32x4*>(p.o + row * D + d) = o;
+    }
+    if (p.lse && d == 0) p.lse[row] = empty ? ninf : 0.69314718055994531f * (m + log2f(l));
+}
+
+template <int D, int BLK>
+hipError_t launch_window_few(const AttnParams& p, hipStream_t st)
+{
+    if (p.mode != kModeDefault) return launch_dec<D, BLK, true, kModeE2E | kModeWindow, false, false, false>(p, st);
+    const hipError_t e = launch_dec<D, BLK, true, kModeDefault | kModeWindow, false, false, false>(p, st);
+    if (e != hipSuccess || p.nsplit == 1) return e;
+    const long long rows = (long long)p.B * p.Hq * p.Sq, per = 256 / (D / 4);
+    hipLaunchKernelGGL((baps_attn_window_combine_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attention_window_few(const AttnParams& p, int D, int block, hipStream_t st)
+{
+    if (D == 64 && block == 32) return launch_window_few<64, 32>(p, st);
+    if (D == 64 && block == 64) return launch_window_few<64, 64>(p, st);
+    if (D == 64 && block == 128) return launch_window_few<64, 128>(p, st);
+    if (D == 128 && block == 32) return launch_window_few<128, 32>(p, st);
+    if (D == 128 && block == 64) return launch_window_few<128, 64>(p, st);
+    if (D == 128 && block == 128) return launch_window_few<128, 128>(p, st);
     return hipErrorInvalidValue;
 }
 

@@ -268,13 +268,17 @@ __device__ __forceinline__ kargs_ptr fresh_args()
 }
 
 // An item's tile, key/value head, batch and key blocks (its last row sees
-// the most keys).
+// the most keys).  A windowed item's nblk blocks are the sinks' nsink first ones
+// and then those from wstart on.
 struct ItemGeo {
     int tile, g, b, nblk;
+    int nsink, wstart;
+    template <bool WIN>
+    __device__ __forceinline__ int block(int j) const { return !WIN || j < nsink ? j : wstart + (j - nsink); }
 };
 
-template <int BLK, int TILE_ROWS>
-__device__ __forceinline__ ItemGeo item_geo(int L, int Hq, int Hkv, int B, int Sq, int Sk, int causal)
+template <int BLK, int TILE_ROWS, bool WIN>
+__device__ __forceinline__ ItemGeo item_geo(int L, int Hq, int Hkv, int B, int Sq, int Sk, int causal, int window, int sinks)
 {
     const int G = Hq / Hkv;
     const int flat_rows = Sq * G;
@@ -283,18 +287,25 @@ __device__ __forceinline__ ItemGeo item_geo(int L, int Hq, int Hkv, int B, int S
     decode_item(L, ntiles, B * Hkv, Hkv, e.tile, e.g, e.b);
     const int f_last = min(flat_rows - 1, e.tile * TILE_ROWS + TILE_ROWS - 1);
     const int kmax_tile = causal ? min(Sk - 1, f_last / G + Sk - Sq) : Sk - 1;
-    e.nblk = kmax_tile < 0 ? 0 : kmax_tile / BLK + 1;
+    if constexpr (WIN) {
+        const KeyBlocks kb = key_blocks<BLK>(e.tile * TILE_ROWS / G + Sk - Sq, kmax_tile, window, sinks);
+        e.nblk = kb.n;
+        e.nsink = kb.nsink;
+        e.wstart = kb.wstart;
+    } else {
+        e.nblk = kmax_tile < 0 ? 0 : kmax_tile / BLK + 1;
+    }
     return e;
 }
 
 // The item a workgroup takes in round r, with its geometry; false past the last
-template <int BLK, int TILE_ROWS>
+template <int BLK, int TILE_ROWS, bool WIN>
 __device__ __forceinline__ bool item_of_round(kargs_ptr a, int r, ItemGeo& e)
 {
     const int ntiles = (a->Sq * (a->Hq / a->Hkv) + TILE_ROWS - 1) / TILE_ROWS;
     const int L = item_at(r, blockIdx.x, gridDim.x, ntiles * a->B * a->Hkv);
     if (L < 0) return false;
-    e = item_geo<BLK, TILE_ROWS>(L, a->Hq, a->Hkv, a->B, a->Sq, a->Sk, a->causal);
+    e = item_geo<BLK, TILE_ROWS, WIN>(L, a->Hq, a->Hkv, a->B, a->Sq, a->Sk, a->causal, WIN ? a->window : 0, WIN ? a->sinks : 0);
     return true;
 }
 
@@ -304,9 +315,14 @@ __device__ __forceinline__ bool item_of_round(kargs_ptr a, int r, ItemGeo& e)
 // table covers the T whose bits 18..0 are zero, the only ones that can sit
 // exactly halfway).  DUMP: also write the raw dot products and the block
 // references of the rows the caller marks (AttnParams::dump_slot).
-template <int D, int BLK, int NW, int KW, bool CT, int MODE, bool TILE, bool F8, bool PERSIST, bool TIE, bool DUMP>
+// MODE_: the softmax setup, with kModeWindow for a windowed call, whose blocks
+// are those that its rows reach.
+template <int D, int BLK, int NW, int KW, bool CT, int MODE_, bool TILE, bool F8, bool PERSIST, bool TIE, bool DUMP>
 __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
 {
+    constexpr int MODE = MODE_ & ~kModeWindow;
+    constexpr bool WIN = (MODE_ & kModeWindow) != 0;
+    static_assert(!WIN || (CT && !TILE && !F8 && !TIE && !DUMP), "windowed calls: per-row restart, bf16 Q/K");
     static_assert(MODE == kModeE2E || CT, "the eq. (2) setups use the compact table (T <= 0)");
     static_assert(MODE == kModeE2E || !TILE, "tile-level restart belongs to Alg. 1");
     static_assert(!TIE || (MODE == kModeE2E && CT && !TILE && !F8), "ties to even: canonical per-row path");
@@ -468,8 +484,8 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
     };
 
     ItemGeo cur;
-    if (!item_of_round<BLK, C::kTileRows>(fresh_args(), 0, cur)) return;   // (the grid holds at most one workgroup per item)
-    if (cur.nblk > 0) issue_block(kv_off(cur), 0, 0);
+    if (!item_of_round<BLK, C::kTileRows, WIN>(fresh_args(), 0, cur)) return;   // (the grid holds at most one workgroup per item)
+    if (cur.nblk > 0) issue_block(kv_off(cur), cur.block<WIN>(0), 0);
     if constexpr (MODE != kModeDefault) {                  // (Default evaluates exp2 in fp32: no table)
         if constexpr (CT) {
             // asynchronous copy (the LDS address handed to the loads is the
@@ -510,15 +526,25 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
         const int kmax = row_ok ? (p.causal ? min(p.Sk - 1, r + off) : p.Sk - 1) : -1;
         int dslot = -1;
         if constexpr (DUMP) dslot = row_ok ? p.dump_slot[((long long)cur.b * p.Hq + h) * p.Sq + r] : -1;
+        const int kmin = (WIN && row_ok) ? max(0, r + off - p.window + 1) : 0;   // sinks apart
         int kmax_wave_hi = kmax, kmax_wave_lo = row_ok ? kmax : 0x7fffffff;
+        int kmin_wave_hi = kmin, kmin_wave_lo = row_ok ? kmin : 0x7fffffff;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             kmax_wave_hi = max(kmax_wave_hi, __shfl_xor(kmax_wave_hi, o, 64));
             kmax_wave_lo = min(kmax_wave_lo, __shfl_xor(kmax_wave_lo, o, 64));
+            if constexpr (WIN) {
+                kmin_wave_hi = max(kmin_wave_hi, __shfl_xor(kmin_wave_hi, o, 64));
+                kmin_wave_lo = min(kmin_wave_lo, __shfl_xor(kmin_wave_lo, o, 64));
+            }
         }
         // wave-uniform from here on: keeps the skip and mask branches scalar
         kmax_wave_hi = __builtin_amdgcn_readfirstlane(kmax_wave_hi);
         kmax_wave_lo = __builtin_amdgcn_readfirstlane(kmax_wave_lo);
+        if constexpr (WIN) {
+            kmin_wave_hi = __builtin_amdgcn_readfirstlane(kmin_wave_hi);
+            kmin_wave_lo = __builtin_amdgcn_readfirstlane(kmin_wave_lo);
+        }
 
         // Alg. 1 state of this lane's row.  The output and the denominator are
         // kept relative to the current block reference ref_j instead of the
@@ -537,7 +563,8 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
 #pragma unroll
         for (int t = 0; t < kDT; ++t) oacc[t] = f32x16{};
 
-        for (int jb = 0; jb < cur.nblk; ++jb, sel ^= 1) {
+        for (int jx = 0; jx < cur.nblk; ++jx, sel ^= 1) {
+            const int jb = cur.block<WIN>(jx);
             const int key0 = jb * BLK + kw * kKT * 32;      // this wave's first key of the block
             const char* kt_lds = tiles + sel * 2 * C::kTileBytes + kw * kKT * 32 * (F8 ? D : C::kRowBytes);
             const char* vt_lds = tiles + (sel * 2 + 1) * C::kTileBytes + kw * kKT * 32 * C::kRowBytes;
@@ -545,16 +572,18 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
             __syncthreads();                                // everyone's did; block jb-1 fully consumed
             // the next block of this item, or the first block of the next
             // item while the last one is computed
-            const bool last = jb + 1 == cur.nblk;
+            const bool last = jx + 1 == cur.nblk;
+            const int jn = WIN ? cur.block<WIN>(jx + 1) : jb + 1;   // the block that comes next
             ItemGeo e_next;
             bool has_next = false;
             bool spread = false;        // block jb + 1 loads between this block's Q^T MFMAs
             if (!last) {
-                spread = kSpread && (jb + 2) * BLK <= p.Sk && key0 <= kmax_wave_hi;
-                if (!spread) issue_block(hoff_cur, jb + 1, sel ^ 1);
+                spread = kSpread && (jn + 1) * BLK <= p.Sk && key0 <= kmax_wave_hi &&
+                         (!WIN || key0 + 32 * kKT > kmin_wave_lo || key0 < p.sinks);
+                if (!spread) issue_block(hoff_cur, jn, sel ^ 1);
             } else if constexpr (PERSIST) {
-                has_next = item_of_round<BLK, C::kTileRows>(fresh_args(), rnd + 1, e_next);
-                if (has_next && e_next.nblk > 0) issue_block(kv_off(e_next), 0, sel ^ 1);
+                has_next = item_of_round<BLK, C::kTileRows, WIN>(fresh_args(), rnd + 1, e_next);
+                if (has_next && e_next.nblk > 0) issue_block(kv_off(e_next), e_next.block<WIN>(0), sel ^ 1);
             }
             // A wave that sees nothing of the block skips it.  In a tile that
             // spans waves it still takes part in the tile's exchange below, with
@@ -562,7 +591,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
             // barrier on one path, and the tile's representative lane counts the
             // block whenever any row of the tile sees it.  With the keys split over
             // waves every wave takes part in the exchange of the row maxima.
-            const bool live = key0 <= kmax_wave_hi;
+            const bool live = key0 <= kmax_wave_hi && (!WIN || key0 + 32 * kKT > kmin_wave_lo || key0 < p.sinks);
             if (!live && !(TILE && xwave) && KW == 1) continue;
 
             f32x16 sacc[kKT];
@@ -601,8 +630,8 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
                     // order of reads, MFMAs and loads is written out)
                     constexpr int kNJ = kNJK + kNJV, kPer = (kNJ + kN - 1) / kN;
                     const uint32_t nk = tiles_lds + (sel ^ 1) * 2 * C::kTileBytes;
-                    const uint64_t ksb = uniform_addr(p.k + hoff_cur + (long long)(jb + 1) * BLK * D);
-                    const uint64_t vsb = uniform_addr(p.v + hoff_cur + (long long)(jb + 1) * BLK * D);
+                    const uint64_t ksb = uniform_addr(p.k + hoff_cur + (long long)jn * BLK * D);
+                    const uint64_t vsb = uniform_addr(p.v + hoff_cur + (long long)jn * BLK * D);
                     u32x4 fr[kKReads];
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -659,6 +688,18 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
             }
             // mask keys past kmax (causal diagonal, ragged tail); key of register
             // i of tile kt: key0 + 32*kt + 8*(i/4) + 4*half + i%4
+            // (windowed: and keys in front of kmin that are no sinks)
+            if (WIN && key0 < kmin_wave_hi && key0 + 32 * kKT > p.sinks) {
+                asm volatile("" ::: "memory");
+                const int lim = kmin - key0 - 4 * half, snk = p.sinks - key0 - 4 * half;
+#pragma unroll
+                for (int kt = 0; kt < kKT; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int k = kt * 32 + 8 * (i / 4) + (i % 4);
+                        sacc[kt][i] = (k < lim) & (k >= snk) ? ninf : sacc[kt][i];
+                    }
+            }
             if (key0 + 32 * kKT - 1 > kmax_wave_lo) {
                 asm volatile("" ::: "memory");          // keep this a real branch (no if-conversion)
                 const int lim = kmax - key0 - 4 * half;
@@ -696,10 +737,10 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
                 // the row maximum over the waves that share these rows: they
                 // then take the same decision, hold the same reference, and
                 // their X and dX partials add at the end
-                if (half == 0) xch[jb & 1][kw][rw * kRowsPerWave + j32] = amax;
+                if (half == 0) xch[jx & 1][kw][rw * kRowsPerWave + j32] = amax;
                 __syncthreads();
 #pragma unroll
-                for (int w = 0; w < KW; ++w) amax = __builtin_fmaxf(amax, xch[jb & 1][w][rw * kRowsPerWave + j32]);
+                for (int w = 0; w < KW; ++w) amax = __builtin_fmaxf(amax, xch[jx & 1][w][rw * kRowsPerWave + j32]);
             }
             float nref;
             if constexpr (MODE == kModeE2E) {
@@ -966,8 +1007,8 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
         // this item's last block); its Q is loaded now, behind the O stores
         // (the first block waits for both)
         ItemGeo nxt;
-        if (!PERSIST || !item_of_round<BLK, C::kTileRows>(a, rnd + 1, nxt)) break;
-        if (cur.nblk == 0 && nxt.nblk > 0) issue_block(kv_off(nxt), 0, sel);
+        if (!PERSIST || !item_of_round<BLK, C::kTileRows, WIN>(a, rnd + 1, nxt)) break;
+        if (cur.nblk == 0 && nxt.nblk > 0) issue_block(kv_off(nxt), nxt.block<WIN>(0), sel);
         if (!q_ready) load_q(a, nxt);
         cur = nxt;
     }
@@ -1019,16 +1060,17 @@ hipError_t launch_one(const AttnParams& p, hipStream_t st)
 template <int D, int BLK, bool CT, int MODE, bool F8, bool TIE, bool DUMP>
 hipError_t launch_rows(const AttnParams& p, hipStream_t st)
 {
+    constexpr bool kAlg1 = (MODE & ~kModeWindow) == kModeE2E;
     if constexpr (BLK >= 64) {
         int ncu = 0;
         const hipError_t e = cu_count(&ncu);
         if (e != hipSuccess) return e;
         const PrefillForm f = prefill_form(PrefillShape{D, BLK, p.Sq, p.Sk, p.Hq / p.Hkv, (long long)p.Hkv * p.B,
-                                                        p.causal != 0, F8, MODE == kModeE2E, !CT, TIE, ncu});
+                                                        p.causal != 0, F8, kAlg1, !CT, TIE, ncu});
         if (f.nw == 4 && f.kw == 2) return launch_one<D, BLK, 4, 2, CT, MODE, false, F8, TIE, DUMP>(p, st);
         if constexpr (D * BLK == 16384)
             if (f.kw == 2) return launch_one<D, BLK, 8, 2, CT, MODE, false, F8, TIE, DUMP>(p, st);
-        if constexpr (CT && MODE == kModeE2E && !TIE && (D * BLK == 8192 || (F8 && D * BLK < 8192)))
+        if constexpr (CT && kAlg1 && !TIE && (D * BLK == 8192 || (F8 && D * BLK < 8192)))
             if (f.nw == 4) return launch_one<D, BLK, 4, 1, CT, MODE, false, F8, TIE, DUMP>(p, st);
     }
     return launch_one<D, BLK, 8, 1, CT, MODE, false, F8, TIE, DUMP>(p, st);
@@ -1042,7 +1084,7 @@ hipError_t launch_d_blk(const AttnParams& p, hipStream_t st)
     // in its 16 rows
     const int G = p.Hq / p.Hkv;
     const long long flat = (long long)p.Sq * G;
-    if (flat <= 64 && (long long)p.restart_rows * G <= 16) return launch_attention_decode(p, D, BLK, st);
+    if (flat <= kFewFlatRows && (long long)p.restart_rows * G <= 16) return launch_attention_decode(p, D, BLK, st);
     if (p.tie_even)                                // ties to even (canonical per-row path only)
         return launch_rows<D, BLK, true, kModeE2E, false, true, DUMP>(p, st);
     if (p.qk_f8) {                                 // FP8 Q/K (per-row restart only)

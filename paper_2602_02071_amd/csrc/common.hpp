@@ -101,6 +101,8 @@ __device__ __forceinline__ float exp2_nonpos_int(float k)
 constexpr int kModeE2E = 0;
 constexpr int kModeDefault = 1;
 constexpr int kModeExp2 = 2;
+// The kernels' MODE of a windowed call: the setup with this bit set
+constexpr int kModeWindow = 8;
 
 struct AttnParams {
     const uint16_t* q;          // [B, Hq, Sq, D] bf16
@@ -135,7 +137,35 @@ struct AttnParams {
     float* dump_acc;
     float* dump_ref;
     int dump_nblk;
+    // Windowed calls (kernels built with kModeWindow): the row at position t
+    // sees key c <= t when c > t - window or c < sinks
+    int window, sinks;
+    // and in the Default setup with few rows the keys may be split over nsplit
+    // workgroups: [nsplit][B*Hq*Sq] unnormalised sums and (maximum, sum) pairs
+    int nsplit;
+    float* part;                // [..][D]
+    float* ml;                  // [..][2]
 };
+
+// Key blocks of KB keys that the rows at positions t_lo .. t_hi reach: the
+// sinks' blocks first, then the window's, as one list of n blocks.  window 0:
+// every key up to the row.
+struct KeyBlocks {
+    int nsink, wstart, n, lo;       // lo: the first key of the window of the lowest row
+    __device__ __forceinline__ int block(int j) const { return j < nsink ? j : wstart + (j - nsink); }
+};
+
+template <int KB>
+__device__ __forceinline__ KeyBlocks key_blocks(int t_lo, int t_hi, int window, int sinks)
+{
+    KeyBlocks r;
+    r.lo = window > 0 ? max(0, t_lo - window + 1) : 0;
+    const int ns = min(min(sinks, r.lo), t_hi + 1);             // sink keys in front of the window
+    r.wstart = r.lo / KB;
+    r.nsink = ns > 0 ? min((ns + KB - 1) / KB, r.wstart) : 0;
+    r.n = t_hi < 0 ? 0 : r.nsink + (t_hi / KB - r.wstart + 1);
+    return r;
+}
 
 struct SoftmaxBlockParams {
     const float* s;
@@ -244,5 +274,9 @@ hipError_t launch_attention(const AttnParams& p, int D, int block, hipStream_t s
 hipError_t launch_attention_dump(const AttnParams& p, int D, int block, hipStream_t st);
 hipError_t launch_attention_decode(const AttnParams& p, int D, int block, hipStream_t st);
 hipError_t launch_attention_split(const SplitParams& sp, int D, int block, hipStream_t st);
+hipError_t launch_attention_window(const AttnParams& p, int D, int block, hipStream_t st);
+hipError_t launch_attention_window_few(const AttnParams& p, int D, int block, hipStream_t st);
+// rows per key/value head up to which a call takes the few-rows kernel
+constexpr long long kFewFlatRows = 64;
 
 }  // namespace baps
