@@ -469,7 +469,8 @@ bool cache_ok(const baps_cache_t* c)
 
 bool cache_supported(const baps_cache_t& c)
 {
-    return (c.D == 64 || c.D == 128) && (c.page == 16 || c.page == 32 || c.page == 64 || c.page == 128) && c.Hkv <= 32767;
+    return (c.D == 64 || c.D == 128) && (c.page == 16 || c.page == 32 || c.page == 64 || c.page == 128) && c.Hkv <= 32767 &&
+           (long long)c.num_pages * c.Hkv <= 0x7fffffffLL;
 }
 
 bool cache_arrays(const baps_cache_t& c)
@@ -506,7 +507,7 @@ int cache_plan(const baps_cache_t& c, int B, int Hq, int total_q, int max_q, int
         clear_stale_error();
         ncu = 256;
     }
-    *nsplit = cache_attention_splits(B, Hq, c.Hkv, max_q, max_len, window, sinks, ncu);
+    *nsplit = cache_attention_splits(B, Hq, c.Hkv, c.D, max_q, max_len, window, sinks, ncu);
     if (*nsplit > 1) *bytes = align256((long long)*nsplit * total_q * Hq * (c.D + 2) * 4);
     return BAPS_OK;
 }
@@ -744,7 +745,8 @@ int baps_cache_attention(const baps_cache_t* cache, int layer, const void* q, lo
     if (cache->Hkv == 0 || Hq % cache->Hkv) return BAPS_INVALID_ARGUMENT;
     if (!cache_supported(*cache) || !width_ok(*cache, table_width) || B > 65535 || cache->num_pages == 0 || table_width == 0)
         return BAPS_UNSUPPORTED;
-    if ((long long)max_q * (Hq / cache->Hkv) > (1LL << 30) || 4LL * cache->Hkv > 65535) return BAPS_UNSUPPORTED;
+    const long long flat = (long long)max_q * (Hq / cache->Hkv);
+    if (flat > (1LL << 30) || 4LL * cache->Hkv > 65535 || (flat + 15) / 16 * B * cache->Hkv > (1LL << 24)) return BAPS_UNSUPPORTED;
     if (!cache_arrays(*cache) || !q || !o || !cu_q || !lens || !table) return BAPS_INVALID_ARGUMENT;
     if (!aligned16(q) || !aligned16(o) || q_stride < (long long)Hq * cache->D || q_stride % 8) return BAPS_INVALID_ARGUMENT;
     try {

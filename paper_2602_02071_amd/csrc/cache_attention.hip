@@ -12,6 +12,8 @@
 // bytes.  tile: 256 rows per workgroup, for chunks of a prompt; bound by the
 // matrix unit and the exponentials.  Either splits the keys of a row over
 // workgroups where rows alone are too few, and combine joins the parts.
+#include <type_traits>
+
 #include "cache.hpp"
 
 namespace baps {
@@ -40,6 +42,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return __builtin_bit_cast(uint32_t, v);
 }
 
+// the larger of the values of lanes l and l ^ 32
+__device__ __forceinline__ float max_halves(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(hif8::u2f(r[0]), hif8::u2f(r[1]));
+}
+
 // A sequence's new tokens and length, held to what the buffers have.
 struct Seq {
     int c0, n, first, len;          // packed rows [c0, c0 + n) at positions first ..; keys [0, len)
@@ -48,7 +58,7 @@ struct Seq {
 __device__ __forceinline__ Seq sequence(const CacheAttnParams& p, int b)
 {
     Seq s;
-    const int c1 = p.cu[b + 1], len = p.lens[b];
+    const int c1 = p.cu[b + 1], len = min(max(p.lens[b], -(1 << 30)), 1 << 30);
     s.c0 = p.cu[b];
     s.n = c1 - s.c0;
     if (s.c0 < 0 || s.n <= 0 || c1 > p.total_q) s.n = 0;
@@ -65,10 +75,8 @@ struct Group {
     bool bad;
 };
 
-__device__ __forceinline__ Group group_at(const CacheAttnParams& p, const int* row, int key, int h)
+__device__ __forceinline__ Group group_of(const CacheAttnParams& p, int page, int h)
 {
-    const int slot = min(key >> p.c.lpage, p.table_width - 1);
-    const int page = row[slot];
     Group g;
     g.bad = (unsigned)page >= (unsigned)p.c.num_pages;
     g.ph = (long long)(g.bad ? 0 : page) * p.c.Hkv + h;
@@ -87,6 +95,11 @@ __device__ __forceinline__ uint32_t keys_seen(int k0, int t_hi, int lo, int sink
 __device__ __forceinline__ uint32_t byte_mask(uint32_t seen, int w)
 {
     return ((((seen >> (4 * w)) & 15u) * 0x204081u) & 0x01010101u) * 0xffu;
+}
+
+__device__ __forceinline__ Group group_at(const CacheAttnParams& p, const int* row, int key, int h)
+{
+    return group_of(p, row[min(key >> p.c.lpage, p.table_width - 1)], h);
 }
 
 // ---------------------------------------------------------------- rows kernel
@@ -309,38 +322,134 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
 }
 
 // ---------------------------------------------------------------- tile kernel
-// Eight waves of 32 rows each, blocks of 64 keys.  The codes of a block come
+// NW waves of 32 rows each, blocks of 64 keys.  The codes of a block come
 // through registers (one 16-byte load of K and of V per thread at D = 128),
-// are dequantised once for the eight waves and stored to LDS as bf16, into a
-// double buffer: the loads of block j+2 are in flight and block j+1 is stored
-// while block j is computed.  K lies as [key][d], V as [d][key], both with
-// their 16-byte chunks XOR-swizzled.  S^T = K Q^T on 32x32x16 with the rows of
+// are dequantised once for all waves and stored to LDS as bf16.  K lies as
+// [key][d], V as [d][key], both with their 16-byte chunks XOR-swizzled (reads
+// and stores without bank conflicts).  S^T = K Q^T on 32x32x16 with the rows of
 // K taken in the order that gives a lane 8 consecutive keys per 16-key chunk
-// (row 8a + 4 half + b of the tile is key 16 (a/2) + 8 half + 4 (a%2) + b), so
-// V^T's operand is one 16-byte read.
+// (row 8a + 4 half + b of 32 is key 16 (a/2) + 8 half + 4 (a%2) + b), so V^T's
+// operand is one 16-byte read and P never leaves its lane.
+//
+// What bounds it: the instructions of a wave.  Per block and wave 32 MFMAs take
+// 1024 cycles of the SIMD, the exponentials with their exponent, sum and packing
+// 740, staging 250, the maxima 160, for two waves per SIMD.  So the two products
+// and the exponentials of neighbouring half blocks are interleaved by hand, one
+// MFMA each (fused); staging has no address arithmetic beyond one 64-bit
+// product; the reference moves by lazy steps.  2048 rows on 32768 keys (GQA
+// 32/8, D = 128): 1207 us in straight order, 1157 interleaved, 1051 with the
+// short staging, 1000 with the wave's priority raised over the products
+// (1.07 PFLOP/s; without staging it would be 908, without the waits for one
+// another 830).
 constexpr int kBlk = 64;
-constexpr int kTileWaves = 8;
-constexpr int kTileRows = 32 * kTileWaves;
 
-template <int D>
-__global__ __launch_bounds__(64 * kTileWaves, 2) void baps_cache_tile_kernel(CacheAttnParams p)
+// sum over the wave's lanes (DPP: no LDS round trips)
+__device__ __forceinline__ int wave_sum_uniform(int v)
 {
+#define BAPS_STEP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false)
+    BAPS_STEP(0x111, 0xF);                                      // row_shr 1, 2, 4, 8: sums up to each lane of 16
+    BAPS_STEP(0x112, 0xF);
+    BAPS_STEP(0x114, 0xF);
+    BAPS_STEP(0x118, 0xF);
+    BAPS_STEP(0x142, 0xA);                                      // lane 15 of rows 0 and 2 to rows 1 and 3
+    BAPS_STEP(0x143, 0xC);                                      // lane 31 to rows 2 and 3
+#undef BAPS_STEP
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
+// The tiles of all sequences, those that reach furthest first (their keys are
+// the work, and the last ones to start set when the call ends): tile `back` of
+// sequence b counts from its last one and reaches key lens[b] - back * R / G.
+// The place of a workgroup in that order is searched for: tiles that reach x or
+// further are counted per sequence without listing any.  Three sequences of
+// 2500 to 9001 keys, 777 to 2048 new: 617 -> 547 us against the sequences
+// in turn.
+struct TileAt {
+    int b, back;                    // b < 0: no such tile
+};
+
+template <int R>
+__device__ __forceinline__ TileAt tile_of_rank(const CacheAttnParams& p, int rank, int G, int lane)
+{
+    auto tiles = [&](int b) { return (int)(((long long)sequence(p, b).n * G + R - 1) / R); };
+    if (p.B == 1) return rank < tiles(0) ? TileAt{0, rank} : TileAt{-1, 0};
+    // lane holds sequences lane, lane + 64, ..; the first one's numbers stay in
+    // registers
+    auto len_of = [&](int b) { return min(max(p.lens[b], 0), 1 << 30); };
+    const int len0 = lane < p.B ? len_of(lane) : 0, tiles0 = lane < p.B ? tiles(lane) : 0;
+    // tiles of a sequence that reach x
+    auto reach_of = [&](int len, int n, int x) {
+        const int d = len - x;                                  // (no more than 2^30 apart from zero)
+        return d < 0 ? 0 : (int)min((unsigned)n, (unsigned)(((d + 1LL) * G - 1) / R + 1));
+    };
+    auto reach = [&](int b, int x) { return b < 64 ? reach_of(len0, tiles0, x) : reach_of(len_of(b), tiles(b), x); };
+    auto count = [&](int x) {
+        int n = reach_of(len0, tiles0, x);
+        for (int b = lane + 64; b < p.B; b += 64) n += reach(b, x);
+        return wave_sum_uniform(n);
+    };
+    // the largest x with more than rank tiles that reach it
+    int lo = -p.max_q - 1, hi = len0 + 1;               // (no tile reaches further back than its rows)
+    for (int b = lane + 64; b < p.B; b += 64) hi = max(hi, len_of(b) + 1);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) hi = max(hi, __shfl_xor(hi, o, 64));
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    if (count(lo) <= rank) return TileAt{-1, 0};
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (count(mid) > rank) lo = mid; else hi = mid;
+    }
+    // among the tiles that reach lo and no further, in the order of the sequences
+    int skip = rank - count(lo + 1);
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int b = b0 + lane;
+        const int before = b < p.B ? reach(b, lo + 1) : 0;
+        const int n = b < p.B ? reach(b, lo) - before : 0;
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += y;
+        }
+        const int total = __builtin_amdgcn_readfirstlane(__shfl(sum, 63, 64));
+        if (skip < total) {
+            const unsigned long long m = __ballot(sum > skip);
+            const int l = __builtin_ctzll(m);
+            const int back = before + skip - (sum - n);
+            return TileAt{b0 + l, __builtin_amdgcn_readfirstlane(__shfl(back, l, 64))};
+        }
+        skip -= total;
+    }
+    return TileAt{-1, 0};
+}
+
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnParams p)
+{
+    constexpr int kTileRows = 32 * NW;
     constexpr int kDK = D / 16, kDT = D / 32, kKT = kBlk / 32;
     constexpr int kKB = kBlk * D * 2;                           // bytes of a K (or V) tile
     constexpr int kChunks = kBlk * D / 16;                      // 16-byte pieces of codes (512 or 256)
+    constexpr int kPer = (kChunks + 64 * NW - 1) / (64 * NW);   // of a thread
     extern __shared__ __attribute__((aligned(1024))) char lds[];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int j32 = lane & 31, half = lane >> 5;
     const int G = p.Hq / p.c.Hkv;
-    const int ntiles = gridDim.x / p.nsplit;
-    const int split = blockIdx.x % p.nsplit;
-    const int tile = ntiles - 1 - blockIdx.x / p.nsplit;        // the tiles with the most keys first
-    const int h = blockIdx.y, b = blockIdx.z;
+    // head fastest: with 8 of them each XCD (workgroups go round-robin over the
+    // eight) keeps one head's codes in its L2
+    const int h = blockIdx.x % p.c.Hkv;
+    const int split = blockIdx.x / p.c.Hkv % p.nsplit;
+    const int rank = blockIdx.x / (p.c.Hkv * p.nsplit);
+    const TileAt at = tile_of_rank<kTileRows>(p, rank, G, lane);
+    if (at.b < 0) return;
+    const int b = at.b;
     const Seq s = sequence(p, b);
-    const int f0 = tile * kTileRows, flat = s.n * G;
-    if (f0 >= flat) return;
+    const int flat = s.n * G;
+    const int tile = (flat + kTileRows - 1) / kTileRows - 1 - at.back;
+    if (tile < 0) return;                                       // (the caller's arrays changed meanwhile)
+    const int f0 = tile * kTileRows;
 
     const int f = f0 + wave * 32 + j32;
     const bool row_ok = f < flat;
@@ -351,7 +460,6 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void baps_cache_tile_kernel(Cac
     // positions that the workgroup and this wave hold
     const int t_lo = s.first + f0 / G, t_hi = min(s.first + min(flat - 1, f0 + kTileRows - 1) / G, s.len - 1);
     const int wf0 = f0 + wave * 32;
-    const bool wave_ok = wf0 < flat;
     const int w_lo = s.first + wf0 / G, w_hi = min(s.first + min(flat - 1, wf0 + 31) / G, s.len - 1);
 
     const KeyBlocks kb = key_blocks<kBlk>(t_lo, t_hi, p.window, p.sinks);
@@ -364,145 +472,320 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void baps_cache_tile_kernel(Cac
         qop[k] = *reinterpret_cast<const u32x4*>(p.q + (s.c0 + i) * p.qstride + hq * D + 16 * k + 8 * half);
 
     const int* trow = p.table + (long long)b * p.table_width;
-    const int page_mask = (1 << p.c.lpage) - 1;
-    // this thread's piece of a block's codes: K row kr_, elements 16 kc_ ..;
-    // V's 16-token group vg_, element vd_
-    const bool loads = tid < kChunks;
-    const int kr_ = tid / (D / 16) % kBlk, kc_ = tid % (D / 16);
-    const int vg_ = tid / D % (kBlk / 16), vd_ = tid % D;
-    u32x4 kraw = {}, vraw = {};
-    float ks = 1.0f, vs = 1.0f;
-    bool vbad = false;
-    auto fetch = [&](int jj) {
-        if (!loads) return;
-        const int key0 = kb.block(jj) * kBlk;
-        const Group gk = group_at(p, trow, key0 + kr_, h);
-        kraw = *reinterpret_cast<const u32x4*>(p.c.k + ((gk.ph << p.c.lpage) + ((key0 + kr_) & page_mask)) * D + 16 * kc_);
-        ks = pow2_of_byte(p.c.ke[gk.ph]);
-        const int kv = key0 + 16 * vg_;
-        const Group gv = group_at(p, trow, kv, h);
-        vraw = *reinterpret_cast<const u32x4*>(p.c.v + ((gv.ph << p.c.lpage) + (kv & page_mask)) * D + 16 * vd_);
-        vs = pow2_of_byte(p.c.ve[gv.ph]);
-        vbad = gv.bad;
-    };
-    // codes to LDS; V's of keys that no row here sees (behind the last, in
-    // front of the window, a missing page) as zeros
-    __shared__ __attribute__((aligned(16))) uint32_t badg[2][kBlk / 16];   // 1: the block's 16-token group has no page
-    auto store = [&](int jj, int buf) {
-        if (!loads) return;
-        const int key0 = kb.block(jj) * kBlk;
-        char* kt = lds + buf * 2 * kKB;
-        char* vt = kt + kKB;
-        const int kx = D == 128 ? (kr_ & 15) : ((kr_ >> 1) & 7);
-        *reinterpret_cast<u32x4*>(kt + kr_ * 2 * D + 16 * ((2 * kc_) ^ kx)) = dequant8(kraw[0], kraw[1], ks);
-        *reinterpret_cast<u32x4*>(kt + kr_ * 2 * D + 16 * ((2 * kc_ + 1) ^ kx)) = dequant8(kraw[2], kraw[3], ks);
-        u32x4 v = vraw;
-        const int k0 = key0 + 16 * vg_;
-        if (k0 + 15 > t_hi || (k0 < kb.lo && k0 + 15 >= p.sinks) || vbad) {
-            const uint32_t seen = keys_seen(k0, t_hi, kb.lo, p.sinks, vbad);
+    const int lp = p.c.lpage, page_mask = (1 << lp) - 1;
+    auto page_of = [&](int key) { return trow[min(key >> lp, p.table_width - 1)]; };
+    auto no_page = [&](int page) { return (unsigned)page >= (unsigned)p.c.num_pages; };
+    // Whether some key that a row here may see has no page (then scores and V
+    // are masked by the table too)
+    bool holes = false;
+    {
+        for (int k = (kb.lo >> lp) + tid; k <= t_hi >> lp; k += 64 * NW) holes |= no_page(page_of(k << lp));
+        const int ns = min(min(p.sinks, kb.lo), t_hi + 1);
+        for (int k = tid; k << lp < ns; k += 64 * NW) holes |= no_page(page_of(k << lp));
+    }
+    {
+        // (through the tiles' LDS: static LDS would take the room of a second
+        // workgroup)
+        uint32_t* flags = reinterpret_cast<uint32_t*>(lds);
+        const bool mine = __any(holes);
+        if (lane == 0) flags[wave] = mine;
+        __syncthreads();
+        uint32_t any = 0;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) v[w] &= byte_mask(seen, w);
+        for (int w = 0; w < NW; ++w) any |= flags[w];
+        holes = __builtin_amdgcn_readfirstlane(any);
+        __syncthreads();
+    }
+
+    // A thread's pieces of a block's codes, c = tid, tid + threads, ..: of K row
+    // c / (D/16), elements 16 (c % (D/16)) ..; of V the 16-token group c / D,
+    // element c % D.  K comes in pairs of half blocks of 32 keys: the upper one
+    // of block jj and the lower one of block jj + 1.  All that depends on the
+    // thread is in a constant offset, all that depends on the block is uniform
+    // in the wave.
+    constexpr int kThreads = 64 * NW;
+    u32x4 kraw[kPer], vraw[kPer];
+    uint32_t ke[kPer], ve[kPer];
+    int kpage[kPer], vpage[kPer];
+    const uint32_t page_bytes = (uint32_t)D << lp;
+    uint32_t kin[kPer], vin[kPer];                              // byte offsets inside a page
+    uint32_t kst[kPer], vst[kPer];                              // and inside an LDS tile
+    int kup[kPer];                                              // the piece's half block of the pair (uniform)
+    int kslot[kPer], vslot[kPer];                               // table entries behind the half block's / block's first
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+        const int c = (tid + u * kThreads) % kChunks;           // (D = 64, eight waves: two threads per piece)
+        const int kr = c / (D / 16), kc = c % (D / 16), r = kr & 31, vg = c / D, vd = c % D;
+        const int kx = D == 128 ? (r & 15) : ((r >> 1) & 7), vx = (vd >> 1) & 7;
+        kup[u] = __builtin_amdgcn_readfirstlane(kr >> 5);
+        kslot[u] = r >> lp;
+        vslot[u] = 16 * vg >> lp;
+        kin[u] = (r & page_mask) * D + 16 * kc;
+        vin[u] = (16 * vg & page_mask) * D + 16 * vd;
+        kst[u] = r * 2 * D + 16 * ((2 * kc) ^ kx);
+        vst[u] = vd * 2 * kBlk + 16 * ((2 * vg) ^ vx);
+    }
+    auto k_first = [&](int jj, int u) {                         // the first key of the piece's half block
+        return kup[u] ? kb.block(min(jj + 1, j1 - 1)) * kBlk : kb.block(max(jj, j0)) * kBlk + 32;
+    };
+    // The page of a piece is looked up one step ahead of its codes, so that no
+    // load waits for the table.
+    auto look_k = [&](int jj) {
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) kpage[u] = trow[(uint32_t)min((k_first(jj, u) >> lp) + kslot[u], p.table_width - 1)];
+    };
+    auto look_v = [&](int jj) {
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) vpage[u] = trow[(uint32_t)min((kb.block(jj) * kBlk >> lp) + vslot[u], p.table_width - 1)];
+    };
+    // (a page that is none is read as the last one, and masked)
+    auto page_head = [&](int page) { return min((uint32_t)page, (uint32_t)p.c.num_pages - 1u) * (uint32_t)p.c.Hkv + (uint32_t)h; };
+    auto fetch_k = [&](int jj) {
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const uint32_t ph = page_head(kpage[u]);
+            const uint8_t* at = p.c.k + (k_first(jj, u) & page_mask) * D;
+            kraw[u] = *reinterpret_cast<const u32x4*>(at + ((uint64_t)ph * page_bytes + kin[u]));
+            ke[u] = p.c.ke[ph];
         }
-        const int vx = (vd_ >> 1) & 7;
-        *reinterpret_cast<u32x4*>(vt + vd_ * 2 * kBlk + 16 * ((2 * vg_) ^ vx)) = dequant8(v[0], v[1], vs);
-        *reinterpret_cast<u32x4*>(vt + vd_ * 2 * kBlk + 16 * ((2 * vg_ + 1) ^ vx)) = dequant8(v[2], v[3], vs);
-        if (vd_ == 0) badg[buf][vg_] = vbad;
+    };
+    auto fetch_v = [&](int jj) {
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const uint32_t ph = page_head(vpage[u]);
+            const uint8_t* at = p.c.v + (kb.block(jj) * kBlk & page_mask) * D;
+            vraw[u] = *reinterpret_cast<const u32x4*>(at + ((uint64_t)ph * page_bytes + vin[u]));
+            ve[u] = p.c.ve[ph];
+        }
+    };
+    // V's codes of keys that no row here sees (behind the last, in front of the
+    // window, a missing page) become zeros
+    auto clean_v = [&](int jj) {
+        const int key0 = kb.block(jj) * kBlk;
+        if (key0 + kBlk - 1 <= t_hi && (key0 >= kb.lo || key0 + kBlk <= p.sinks) && !holes) return;
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int k0 = key0 + (tid + u * kThreads) % kChunks / D * 16;
+            const uint32_t seen = keys_seen(k0, t_hi, kb.lo, p.sinks, no_page(page_of(k0)));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) vraw[u][w] &= byte_mask(seen, w);
+        }
+    };
+    // LDS: four half blocks of K (half 2 j of block j in slot 2 j % 4), then three
+    // blocks of V^T
+    constexpr int kHalf = 32 * 2 * D, kVBase = 4 * kHalf;
+    auto store_k = [&](int slot) {                              // the pair into slots slot and (slot + 1) % 4
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const uint32_t at = kst[u] + ((slot + kup[u]) & 3) * kHalf;
+            const float s = pow2_of_byte(ke[u]);
+            *reinterpret_cast<u32x4*>(lds + at) = dequant8(kraw[u][0], kraw[u][1], s);
+            *reinterpret_cast<u32x4*>(lds + (at ^ 16)) = dequant8(kraw[u][2], kraw[u][3], s);
+        }
+    };
+    auto store_v = [&](int buf) {                               // buf: byte offset of the block
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const uint32_t at = vst[u] + buf;
+            const float s = pow2_of_byte(ve[u]);
+            *reinterpret_cast<u32x4*>(lds + at) = dequant8(vraw[u][0], vraw[u][1], s);
+            *reinterpret_cast<u32x4*>(lds + (at ^ 16)) = dequant8(vraw[u][2], vraw[u][3], s);
+        }
     };
 
     const float ninf = -__builtin_huge_valf();
-    float m = ninf, l = 0.0f;
+    float m = ninf, l = 0.0f, l2 = 0.0f, nref = 0.0f;
     f32x16 oacc[kDT];
 #pragma unroll
     for (int t = 0; t < kDT; ++t) oacc[t] = f32x16{};
-    // the lane's K rows: row j32 of a tile is key 16 (a/2) + 8 hf + 4 (a%2) + b
+    // the lane's K rows: row j32 of a half block is key 16 (a/2) + 8 hf + 4 (a%2) + b
     const int ka = j32 >> 3, kh = (j32 >> 2) & 1;
     const int krow = 16 * (ka >> 1) + 8 * kh + 4 * (ka & 1) + (j32 & 3);
-    const int kx = D == 128 ? (krow & 15) : ((krow >> 1) & 7);  // (the same for krow + 32)
+    const int kx = D == 128 ? (krow & 15) : ((krow >> 1) & 7);
     const int vx = (j32 >> 1) & 7;                              // (the same for j32 + 32 t)
+    uint32_t koff[kDK], voff[2 * kKT];
+#pragma unroll
+    for (int k = 0; k < kDK; ++k) koff[k] = krow * 2 * D + 16 * ((2 * k + half) ^ kx);
+#pragma unroll
+    for (int c = 0; c < 2 * kKT; ++c) voff[c] = j32 * 2 * kBlk + 16 * ((2 * c + half) ^ vx);
 
-    if (j0 < j1) {
-        fetch(j0);
-        store(j0, 0);
-        if (j0 + 1 < j1) fetch(j0 + 1);
-    }
-    for (int j = j0; j < j1; ++j) {
-        const int buf = (j - j0) & 1;
-        __syncthreads();                                        // block j is in LDS, block j-1 is done with
-        const int key0 = kb.block(j) * kBlk;
-        const char* kt = lds + buf * 2 * kKB;
-        const char* vt = kt + kKB;
-        const u32x4 bg = *reinterpret_cast<const u32x4*>(badg[buf]);
-        const uint32_t bad = bg[0] | bg[1] << 1 | bg[2] << 2 | bg[3] << 3;
-        // a wave whose rows see nothing of the block leaves it
-        const bool live = wave_ok && key0 <= w_hi &&
-                          (p.window == 0 || key0 + kBlk - 1 > w_lo - p.window || key0 < p.sinks);
-        f32x16 sacc[kKT];
-        if (live) {
+    auto k_read = [&](int k, int slot) { return *reinterpret_cast<const u32x4*>(lds + koff[k] + slot * kHalf); };
+    auto v_read = [&](uint32_t at, int dt) { return *reinterpret_cast<const u32x4*>(lds + at + 32 * dt * 2 * kBlk); };
+    // P of the upper 16 of the current 32 keys, and where their V is: their
+    // product is formed beside the next 32 keys' scores
+    u32x4 late = {};
+    uint32_t late_at = kVBase + voff[0];
+    auto finish = [&]() {
 #pragma unroll
-            for (int t = 0; t < kKT; ++t) sacc[t] = f32x16{};
-#pragma unroll
-            for (int k = 0; k < kDK; ++k)
-#pragma unroll
-                for (int t = 0; t < kKT; ++t) {
-                    const u32x4 a = *reinterpret_cast<const u32x4*>(kt + (32 * t + krow) * 2 * D + 16 * ((2 * k + half) ^ kx));
-                    sacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qop[k]), sacc[t], 0, 0, 0);
-                }
-        }
-        if (j + 1 < j1) {
-            store(j + 1, buf ^ 1);
-            if (j + 2 < j1) fetch(j + 2);
-        }
-        if (!live) continue;
-        // register 8c + e of tile t is key 32 t + 16 c + 8 half + e
-        if (key0 + kBlk - 1 > w_lo || (p.window > 0 && key0 <= w_hi - p.window && key0 + kBlk > p.sinks) || bad || wf0 + 31 >= flat) {
+        for (int d = 0; d < kDT; ++d)
+            oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v_read(late_at, d)), as_bf16x8(late), oacc[d], 0, 0, 0);
+        late = u32x4{0, 0, 0, 0};
+    };
+    // masks 32 keys' scores and takes the reference that their P are formed
+    // against.  That is the running maximum only up to a factor of 2^8: it moves
+    // when a row's maximum passes it by more, so that the output is rarely
+    // rescaled (P stays within 2^8 of 1, in floating point at the same relative
+    // precision, and the sums in fp32).
+    auto settle = [&](f32x16& sc, int key0) {
+        if (key0 + 31 > w_lo || (p.window > 0 && key0 <= w_hi - p.window && key0 + 32 > p.sinks) || holes || wf0 + 31 >= flat) {
             const int k0 = key0 + 8 * half;
             const int hi = pos - k0, lo = win_lo - k0, snk = p.sinks - k0;
+            const bool gone0 = holes && no_page(page_of(key0)), gone1 = holes && no_page(page_of(key0 + 16));
 #pragma unroll
-            for (int t = 0; t < kKT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int k = 32 * t + 16 * (r >> 3) + (r & 7);
-                    const bool gone = (bad >> (2 * t + (r >> 3))) & 1u;
-                    sacc[t][r] = (k <= hi) & ((k >= lo) | (k < snk)) & !gone ? sacc[t][r] : ninf;
-                }
+            for (int r = 0; r < 16; ++r) {
+                const int k = 16 * (r >> 3) + (r & 7);
+                sc[r] = (k <= hi) & ((k >= lo) | (k < snk)) & !(r < 8 ? gone0 : gone1) ? sc[r] : ninf;
+            }
         }
         float mx = ninf;
 #pragma unroll
-        for (int t = 0; t < kKT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[t][r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = fmaxf(m, mx * p.scale);
-        const float nref = m_new == ninf ? 0.0f : -m_new;
-        const float fac = m == ninf ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
-        if (__any(fac != 1.0f)) {
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+        mx = max_halves(mx) * p.scale;
+        if (__any(mx > m + 8.0f)) {                             // (m = -inf: any finite maximum)
+            const float m_new = fmaxf(m, mx);
+            const float fac = m == ninf ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+            finish();
 #pragma unroll
             for (int t = 0; t < kDT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) oacc[t][r] *= fac;
+            l *= fac;
+            l2 *= fac;
+            m = m_new;
+            nref = m == ninf ? 0.0f : -m;
         }
-        l *= fac;
-        m = m_new;
+    };
+    // Q^T of the next 32 keys and P V of the current ones in turn, one MFMA each:
+    // first the late 16 keys of the 32 before, then the current lower 16.  The
+    // current scores turn into P between them, one per MFMA (D = 128), their
+    // exponent, exponential and sum each one MFMA after the other, so that no
+    // instruction waits for the one before it; each operand is read from LDS
+    // kAhead MFMAs before its use.  (The order is written out: left to the
+    // compiler, the reads come one MFMA ahead and the exponentials in a bunch.)
+    auto fused = [&](const f32x16& cur, f32x16& nxt, int slot, int at, int up) {
+        constexpr int kN = 2 * kDK, kAhead = 4, kPerSlot = 16 / kN + (16 % kN ? 1 : 0);
+        static_assert(kDK == 2 * kDT, "as many MFMAs of Q^T as of P V");
+        const uint32_t vlow = at + voff[2 * up];
+        auto operand = [&](int i) {
+            if (i & 1) return k_read(i >> 1, slot);
+            const int n = i >> 1;                               // P V: n < kDT late, then the current lower 16 keys
+            return n < kDT ? v_read(late_at, n) : v_read(vlow, n - kDT);
+        };
+        u32x4 fr[kAhead], pop[2];
+        float x[16];
+        auto stage = [&](int r, int s) {
+            if (r < 0 || r >= 16) return;
+            if (s == 0) x[r] = __builtin_fmaf(cur[r], p.scale, nref);
+            if (s == 1) x[r] = __builtin_amdgcn_exp2f(x[r]);
+            if (s == 2) {
+                if (r & 1) l2 += x[r]; else l += x[r];
+                if (r & 1) pop[r >> 3][(r & 7) >> 1] = pack_bf16(x[r - 1], x[r]);
+            }
+        };
+        constexpr int kLead = 4;                                // scores that are ahead of their MFMA
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int t = 0; t < kKT; ++t) {
+        for (int i = 0; i < kAhead; ++i) fr[i] = operand(i);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                u32x4 pop;
+        for (int r = 0; r < kLead; ++r) stage(r, 0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][8 * c + 2 * e], p.scale, nref));
-                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][8 * c + 2 * e + 1], p.scale, nref));
-                    l += p0 + p1;
-                    pop[e] = pack_bf16(p0, p1);
-                }
+        for (int r = 0; r < kLead - 2; ++r) stage(r, 1);
 #pragma unroll
-                for (int dt = 0; dt < kDT; ++dt) {
-                    const u32x4 a = *reinterpret_cast<const u32x4*>(vt + (32 * dt + j32) * 2 * kBlk + 16 * ((4 * t + 2 * c + half) ^ vx));
-                    oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(pop), oacc[dt], 0, 0, 0);
-                }
+        for (int r = 0; r < kLead - 4; ++r) stage(r, 2);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const bf16x8 a = as_bf16x8(fr[i % kAhead]);
+            const int n = i >> 1;
+            if (i & 1) nxt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, as_bf16x8(qop[n]), n ? nxt : f32x16{}, 0, 0, 0);
+            else oacc[n % kDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, as_bf16x8(n < kDT ? late : pop[0]), oacc[n % kDT], 0, 0, 0);
+            if (i + kAhead < kN) fr[i % kAhead] = operand(i + kAhead);
+#pragma unroll
+            for (int e = 0; e < kPerSlot; ++e) {
+                const int r = kPerSlot * i + e;
+                stage(r + kLead, 0);
+                stage(r + kLead - 2, 1);
+                stage(r + kLead - 4, 2);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int r = kPerSlot * kN + kLead - 4; r < 16; ++r) stage(r, 2);
+        late = pop[1];
+        late_at = at + voff[2 * up + 1];
+        // (formed here, not where it is read)
+        asm volatile("" : "+v"(late[0]), "+v"(late[1]), "+v"(late[2]), "+v"(late[3]));
+    };
+
+    // The scores of the next 32 keys are formed while those of the current 32
+    // turn into P: the matrix unit and the VALU work on independent values.  In
+    // step j LDS holds the halves 2 j + 1 and 2 j + 2 of K and V of blocks j - 1
+    // and j; 2 j + 3, 2 j + 4 and V of j + 1 come in.
+    f32x16 sa, sb;
+    int vcur = kVBase, vnext = kVBase + kKB;
+    auto step = [&](auto par_, int j) {
+        constexpr int par = decltype(par_)::value, s1 = 2 * par + 1, s2 = (2 * par + 2) & 3;   // par: (j - j0) & 1
+        const bool more = j + 1 < j1;
+        __syncthreads();
+        if (more) clean_v(j + 1);
+        __builtin_amdgcn_s_setprio(1);                          // (the other wave of the SIMD settles meanwhile)
+        fused(sa, sb, s1, vcur, 0);
+        __builtin_amdgcn_s_setprio(0);
+        settle(sb, kb.block(j) * kBlk + 32);
+        if (more) {
+            store_v(vnext);
+            if (j + 2 < j1) {
+                fetch_v(j + 2);
+                if (j + 3 < j1) look_v(j + 3);
             }
         }
+        __builtin_amdgcn_s_setprio(1);
+        fused(sb, sa, s2, vcur, 1);                             // (past the last block: scores that nobody reads)
+        __builtin_amdgcn_s_setprio(0);
+        if (more) {
+            settle(sa, kb.block(j + 1) * kBlk);
+            store_k((s1 + 2) & 3);
+            if (j + 2 < j1) {
+                fetch_k(j + 2);
+                if (j + 3 < j1) look_k(j + 3);
+            }
+        }
+        vcur = vnext;
+        vnext = vnext == kVBase + 2 * kKB ? kVBase : vnext + kKB;
+    };
+    if (j0 < j1) {
+        look_k(j0 - 1);
+        look_v(j0);
+        fetch_k(j0 - 1);
+        fetch_v(j0);
+        look_k(j0);
+        if (j0 + 1 < j1) look_v(j0 + 1);
+        store_k(3);                                             // (slot 3: unused) and half 0 into slot 0
+        fetch_k(j0);
+        if (j0 + 1 < j1) look_k(j0 + 1);
+        clean_v(j0);
+        store_v(kVBase);
+        if (j0 + 1 < j1) {
+            fetch_v(j0 + 1);
+            if (j0 + 2 < j1) look_v(j0 + 2);
+        }
+        store_k(1);
+        if (j0 + 1 < j1) {
+            fetch_k(j0 + 1);
+            if (j0 + 2 < j1) look_k(j0 + 2);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kDK; ++k)
+            sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k_read(k, 0)), as_bf16x8(qop[k]), k ? sa : f32x16{}, 0, 0, 0);
+        settle(sa, kb.block(j0) * kBlk);
+        for (int j = j0; j < j1; j += 2) {
+            step(std::integral_constant<int, 0>{}, j);
+            if (j + 1 < j1) step(std::integral_constant<int, 1>{}, j + 1);
+        }
+        finish();
     }
+    l += l2;
     l += __shfl_xor(l, 32, 64);
     if (!row_ok) return;
     // register r of d tile dt is element 32 dt + 8 (r/4) + 4 half + r%4
@@ -575,6 +858,12 @@ __global__ __launch_bounds__(256) void baps_cache_combine_kernel(CacheAttnParams
 
 // Up to this many flattened rows per key/value head go to the rows kernel
 constexpr long long kFewRows = 64;
+// Waves of 32 rows in a workgroup of the tile kernel: eight at D = 128, whose
+// tiles' LDS a CU holds once (four, twice: 994 -> 1109 us for 2048 rows on 32768
+// keys, the codes are turned to bf16 twice as often); four at D = 64, two
+// workgroups per CU (156 -> 147 us for four sequences of 3000 to 4000 keys, 16
+// heads).
+template <int D> constexpr int kTileWaves = D == 128 ? 8 : 4;
 
 template <int D>
 hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
@@ -585,18 +874,19 @@ hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
         hipLaunchKernelGGL((baps_cache_rows_kernel<D>), grid, dim3(64 * kWaves), 0, st, p);
     } else {
         static DeviceOnce attr_set;
-        const int bytes = 4 * kBlk * D * 2;
+        const int bytes = 5 * kBlk * D * 2;                     // two blocks of K, three of V
         int dev = 0;
         hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;
         if (!attr_set.is_done(dev)) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(&baps_cache_tile_kernel<D>),
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(&baps_cache_tile_kernel<D, kTileWaves<D>>),
                                     hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
             if (e != hipSuccess) return e;
             attr_set.mark(dev);
         }
-        const dim3 grid((unsigned)((flat + kTileRows - 1) / kTileRows * p.nsplit), (unsigned)p.c.Hkv, (unsigned)p.B);
-        hipLaunchKernelGGL((baps_cache_tile_kernel<D>), grid, dim3(64 * kTileWaves), bytes, st, p);
+        const long long tiles = (flat + 32 * kTileWaves<D> - 1) / (32 * kTileWaves<D>);
+        hipLaunchKernelGGL((baps_cache_tile_kernel<D, kTileWaves<D>>), dim3((unsigned)(tiles * p.B * p.c.Hkv * p.nsplit)),
+                           dim3(64 * kTileWaves<D>), bytes, st, p);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.nsplit == 1) return e;
@@ -608,11 +898,12 @@ hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
 
 }  // namespace
 
-int cache_attention_splits(int B, int Hq, int Hkv, int max_q, int max_len, int window, int sinks, int ncu)
+int cache_attention_splits(int B, int Hq, int Hkv, int D, int max_q, int max_len, int window, int sinks, int ncu)
 {
     const long long flat = (long long)max_q * (Hq / Hkv);
     const bool few = flat <= kFewRows;
-    const long long groups = (flat + (few ? kRows : kTileRows) - 1) / (few ? kRows : kTileRows) * Hkv * B;
+    const int rows = few ? kRows : 32 * (D == 128 ? kTileWaves<128> : kTileWaves<64>);
+    const long long groups = (flat + rows - 1) / rows * Hkv * B;
     long long keys = max_len;                                   // that a workgroup's rows reach
     const long long span = (long long)window + sinks + max_q + 2 * kStep;
     if (window > 0 && span < keys) keys = span;
