@@ -763,6 +763,12 @@ int baps_cache_attention(const baps_cache_t* cache, int layer, const void* q, lo
         p.table_width = table_width; p.B = B; p.Hq = Hq; p.total_q = total_q; p.max_q = max_q;
         p.window = window; p.sinks = sinks;
         p.scale = scale_log2 > 0.0f ? scale_log2 : (float)(1.4426950408889634 / std::sqrt((double)cache->D));
+        // K and V that one call streams past the 256 MiB cache in front of memory
+        // are read without leaving them there, when one workgroup reads them (64
+        // sequences of 5000 to 8192 keys, 436 MB: 160 -> 150 us; where they
+        // fit and are read again soon it loses: 157 MB at D = 64, 39 -> 41)
+        const long long reach = window > 0 && (long long)window + sinks + max_q < max_len ? (long long)window + sinks + max_q : max_len;
+        p.once = 2LL * B * reach * cache->Hkv * cache->D > (256LL << 20);
         p.part = static_cast<float*>(workspace);
         p.ml = p.part + (long long)p.nsplit * total_q * Hq * cache->D;
         clear_stale_error();

@@ -16,7 +16,7 @@
 //   - each wave streams its K and V slots through its own LDS ring, filled by
 //     asynchronous global->LDS loads kept RW slots ahead; a slot is consumed
 //     after the vector-memory counter says it landed and refilled right after.
-#include "common.hpp"
+#include "combine.hpp"
 
 namespace baps {
 
@@ -627,33 +627,15 @@ hipError_t launch_attention_decode(const AttnParams& p, int D, int block, hipStr
 
 namespace {
 
-// Joins a row's parts: their common maximum, then the weighted sums in the
-// parts' order.  One row per D/4 lanes.
+// One workgroup per row.
 template <int D>
 __global__ __launch_bounds__(256) void baps_attn_window_combine_kernel(AttnParams p)
 {
-    constexpr int kLanes = D / 4, kPer = 256 / kLanes;
-    const long long rows = (long long)p.B * p.Hq * p.Sq;
-    const long long row = (long long)blockIdx.x * kPer + threadIdx.x / kLanes;
-    const int d = threadIdx.x % kLanes * 4;
-    if (row >= rows) return;
-    const float ninf = -__builtin_huge_valf();
-    float m = ninf, l = 0.0f;
-    for (int k = 0; k < p.nsplit; ++k) m = __builtin_fmaxf(m, p.ml[2 * (k * rows + row)]);
-    f32x4 o = {};
-    for (int k = 0; k < p.nsplit; ++k) {
-        const float mk = p.ml[2 * (k * rows + row)];
-        if (mk == ninf) continue;
-        const float w = __builtin_amdgcn_exp2f(mk - m);
-        l += w * p.ml[2 * (k * rows + row) + 1];
-        const f32x4 x = *reinterpret_cast<const f32x4*>(p.part + (k * rows + row) * D + d);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += w * x[e];
-    }
-    const bool empty = m == ninf;
-    const float inv = empty ? 0.0f : 1.0f / l;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] *= inv;
+    const long long row = blockIdx.x;
+    f32x4 o;
+    float lse;
+    if (!combine_row<D>(p.part, p.ml, p.nsplit, (long long)p.B * p.Hq * p.Sq, row, o, lse)) return;
+    const int d = 4 * threadIdx.x;
     if (p.out_bf16) {
         const bf16x2 lo = {(__bf16)o[0], (__bf16)o[1]}, hi = {(__bf16)o[2], (__bf16)o[3]};
         *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(p.o) + row * D + d) =
@@ -661,7 +643,7 @@ __global__ __launch_bounds__(256) void baps_attn_window_combine_kernel(AttnParam
     } else {
         *reinterpret_cast<f32x4*>(p.o + row * D + d) = o;
     }
-    if (p.lse && d == 0) p.lse[row] = empty ? ninf : 0.69314718055994531f * (m + log2f(l));
+    if (p.lse && d == 0) p.lse[row] = lse;
 }
 
 template <int D, int BLK>
@@ -670,8 +652,7 @@ hipError_t launch_window_few(const AttnParams& p, hipStream_t st)
     if (p.mode != kModeDefault) return launch_dec<D, BLK, true, kModeE2E | kModeWindow, false, false, false>(p, st);
     const hipError_t e = launch_dec<D, BLK, true, kModeDefault | kModeWindow, false, false, false>(p, st);
     if (e != hipSuccess || p.nsplit == 1) return e;
-    const long long rows = (long long)p.B * p.Hq * p.Sq, per = 256 / (D / 4);
-    hipLaunchKernelGGL((baps_attn_window_combine_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((baps_attn_window_combine_kernel<D>), dim3((unsigned)((long long)p.B * p.Hq * p.Sq)), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 

@@ -42,6 +42,7 @@ struct CacheAttnParams {
     int table_width, B, Hq, total_q, max_q;
     int window, sinks;              // window 0: none
     float scale;                    // score scale in log2 units
+    bool once;                      // the cache is read once and does not stay in the caches on the way
     int nsplit;                     // > 1: partial results go to part / ml
     float* part;                    // [nsplit][total_q * Hq][D] unnormalised sums
     float* ml;                      // [nsplit][total_q * Hq][2] running maximum (log2 units) and sum

@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "cache.hpp"
+#include "combine.hpp"
 
 namespace baps {
 
@@ -50,6 +51,14 @@ __device__ __forceinline__ float max_halves(float x)
     return fmaxf(hif8::u2f(r[0]), hif8::u2f(r[1]));
 }
 
+// the larger of the values of lanes l and l ^ 16
+__device__ __forceinline__ float max_quarters(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return fmaxf(hif8::u2f(r[0]), hif8::u2f(r[1]));
+}
+
 // A sequence's new tokens and length, held to what the buffers have.
 struct Seq {
     int c0, n, first, len;          // packed rows [c0, c0 + n) at positions first ..; keys [0, len)
@@ -68,21 +77,6 @@ __device__ __forceinline__ Seq sequence(const CacheAttnParams& p, int b)
     return s;
 }
 
-// A 16-token group of the cache: its page's place for one head, and whether
-// there is such a page (a missing one is read as page 0 and masked).
-struct Group {
-    long long ph;                   // page * Hkv + head
-    bool bad;
-};
-
-__device__ __forceinline__ Group group_of(const CacheAttnParams& p, int page, int h)
-{
-    Group g;
-    g.bad = (unsigned)page >= (unsigned)p.c.num_pages;
-    g.ph = (long long)(g.bad ? 0 : page) * p.c.Hkv + h;
-    return g;
-}
-
 // Of the 16 keys from k0 on, those up to t_hi that are in the window of the
 // lowest row (lo) or sinks, as bits; none where the group has no page.
 __device__ __forceinline__ uint32_t keys_seen(int k0, int t_hi, int lo, int sinks, bool bad)
@@ -95,11 +89,6 @@ __device__ __forceinline__ uint32_t keys_seen(int k0, int t_hi, int lo, int sink
 __device__ __forceinline__ uint32_t byte_mask(uint32_t seen, int w)
 {
     return ((((seen >> (4 * w)) & 15u) * 0x204081u) & 0x01010101u) * 0xffu;
-}
-
-__device__ __forceinline__ Group group_at(const CacheAttnParams& p, const int* row, int key, int h)
-{
-    return group_of(p, row[min(key >> p.c.lpage, p.table_width - 1)], h);
 }
 
 // ---------------------------------------------------------------- rows kernel
@@ -116,13 +105,14 @@ constexpr int kStep = 64;
 constexpr int kRows = 16;
 constexpr int kWaves = 4;
 
-template <int D>
+template <int D, int TR, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAttnParams p)
 {
     constexpr int kJ = D / 64;                                  // 16-byte pieces of a K row per lane
     constexpr int kDT = D / 16;                                 // 16-wide d tiles of O^T
-    __shared__ float ldo[kWaves - 1][kRows][D];
-    __shared__ float ldm[kWaves][kRows], ldl[kWaves][kRows];
+    constexpr int kTile = kRows * TR;
+    __shared__ float ldo[kWaves - 1][kTile][D];
+    __shared__ float ldm[kWaves][kTile], ldl[kWaves][kTile];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -132,79 +122,113 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
     const int h = blockIdx.y % p.c.Hkv, tile = blockIdx.y / p.c.Hkv;
     const int b = blockIdx.z;
     const Seq s = sequence(p, b);
-    const int f0 = tile * kRows, flat = s.n * G;
+    const int f0 = tile * kTile, flat = s.n * G;
     if (f0 >= flat) return;
 
-    const int f = f0 + c16;
-    const bool row_ok = f < flat;
-    const int i = (row_ok ? f : f0) / G, hq = h * G + (row_ok ? f : f0) % G;
-    const int t_lo = s.first + f0 / G, t_hi = min(s.first + min(flat - 1, f0 + kRows - 1) / G, s.len - 1);
-    const int pos = row_ok ? s.first + i : -1;
-    const int win_lo = p.window > 0 ? pos - p.window + 1 : 0;
-    const long long row = (long long)(s.c0 + i) * p.Hq + hq;
+    const int t_lo = s.first + f0 / G, t_hi = min(s.first + min(flat - 1, f0 + kTile - 1) / G, s.len - 1);
+    // the lane's rows: c16 of each of the TR row tiles
+    bool row_ok[TR];
+    int pos[TR];
+    long long row[TR];
+    u32x4 qop[TR][2 * kJ];
+#pragma unroll
+    for (int x = 0; x < TR; ++x) {
+        row_ok[x] = f0 + kRows * x + c16 < flat;
+        const int f = row_ok[x] ? f0 + kRows * x + c16 : f0;
+        const int i = f / G, hq = h * G + f % G;
+        pos[x] = row_ok[x] ? s.first + i : -1;
+        row[x] = (long long)(s.c0 + i) * p.Hq + hq;
+#pragma unroll
+        for (int k = 0; k < 2 * kJ; ++k)
+            qop[x][k] = *reinterpret_cast<const u32x4*>(p.q + (s.c0 + i) * p.qstride + hq * D + 64 * (k >> 1) + 16 * grp + 8 * (k & 1));
+    }
 
     const KeyBlocks kb = key_blocks<kStep>(t_lo, t_hi, p.window, p.sinks);
     const int per = (kb.n + p.nsplit - 1) / p.nsplit;
     const int j1 = min(kb.n, (split + 1) * per);
     int j = split * per + wave;
 
-    u32x4 qop[2 * kJ];
-#pragma unroll
-    for (int k = 0; k < 2 * kJ; ++k)
-        qop[k] = *reinterpret_cast<const u32x4*>(p.q + (s.c0 + i) * p.qstride + hq * D + 64 * (k >> 1) + 16 * grp + 8 * (k & 1));
-
     const int* trow = p.table + (long long)b * p.table_width;
-    const int page_mask = (1 << p.c.lpage) - 1;
+    const int lp = p.c.lpage, page_mask = (1 << lp) - 1;
+    const uint32_t page_bytes = (uint32_t)D << lp;
     const float ninf = -__builtin_huge_valf();
-    float m = ninf, l = 0.0f;
-    f32x4 oacc[kDT];
+    float m[TR], l[TR];
+    f32x4 oacc[TR][kDT];
 #pragma unroll
-    for (int t = 0; t < kDT; ++t) oacc[t] = f32x4{};
+    for (int x = 0; x < TR; ++x) {
+        m[x] = ninf;
+        l[x] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < kDT; ++t) oacc[x][t] = f32x4{};
+    }
 
+    // The lane's 16-token group of a step is c16 / 4 in K and grp in V; what
+    // depends on the lane is a constant offset into the page.  The page is looked
+    // up one step ahead of its codes, so that no load waits for the table.
+    const int kslot = 16 * (c16 >> 2) >> lp, vslot = 16 * grp >> lp;
+    const uint32_t kin = ((16 * (c16 >> 2) & page_mask) + (c16 & 3)) * D + 16 * grp;
+    const uint32_t vin = (16 * grp & page_mask) * D + 16 * c16;
     u32x4 kr[4][kJ], vr[kDT];
-    float ks = 1.0f, vs = 1.0f;
-    bool bad = false, bad_n = false;
+    uint32_t ke = 0, ve = 0;
+    int kpage = 0, vpage = 0;
+    bool bad_n = false;
+    auto look = [&](int jj, int slot) { return trow[(uint32_t)min((kb.block(jj) * kStep >> lp) + slot, p.table_width - 1)]; };
+    // (a page that is none is read as the last one, and masked)
+    auto page_head = [&](int page) { return min((uint32_t)page, (uint32_t)p.c.num_pages - 1u) * (uint32_t)p.c.Hkv + (uint32_t)h; };
+    auto load16 = [](const uint8_t* at) {
+        const u32x4* q = reinterpret_cast<const u32x4*>(at);
+        return ONCE ? __builtin_nontemporal_load(q) : *q;
+    };
     auto load_k = [&](int jj) {
-        const int key = kb.block(jj) * kStep + 16 * (c16 >> 2);
-        const Group g = group_at(p, trow, key, h);
-        const uint8_t* at = p.c.k + ((g.ph << p.c.lpage) + (key & page_mask) + (c16 & 3)) * D + 16 * grp;
+        const uint32_t ph = page_head(kpage);
+        const uint8_t* at = p.c.k + (kb.block(jj) * kStep & page_mask) * D + ((uint64_t)ph * page_bytes + kin);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int k = 0; k < kJ; ++k) kr[t][k] = *reinterpret_cast<const u32x4*>(at + 4 * t * D + 64 * k);
-        ks = pow2_of_byte(p.c.ke[g.ph]);
+            for (int k = 0; k < kJ; ++k) kr[t][k] = load16(at + 4 * t * D + 64 * k);
+        ke = p.c.ke[ph];
     };
     auto load_v = [&](int jj) {
-        const int key = kb.block(jj) * kStep + 16 * grp;
-        const Group g = group_at(p, trow, key, h);
-        const uint8_t* at = p.c.v + ((g.ph << p.c.lpage) + (key & page_mask)) * D + 16 * c16;
+        const uint32_t ph = page_head(vpage);
+        const uint8_t* at = p.c.v + (kb.block(jj) * kStep & page_mask) * D + ((uint64_t)ph * page_bytes + vin);
 #pragma unroll
-        for (int t = 0; t < kDT; ++t) vr[t] = *reinterpret_cast<const u32x4*>(at + 256 * t);
-        vs = pow2_of_byte(p.c.ve[g.ph]);
-        bad_n = g.bad;
+        for (int t = 0; t < kDT; ++t) vr[t] = load16(at + 256 * t);
+        ve = p.c.ve[ph];
+        bad_n = (unsigned)vpage >= (unsigned)p.c.num_pages;
     };
     if (j < j1) {
+        kpage = look(j, kslot);
+        vpage = look(j, vslot);
         load_k(j);
         load_v(j);
+        if (j + kWaves < j1) {
+            kpage = look(j + kWaves, kslot);
+            vpage = look(j + kWaves, vslot);
+        }
     }
     for (; j < j1; j += kWaves) {
         const int key0 = kb.block(j) * kStep;
-        const bool more = j + kWaves < j1;
-        bad = bad_n;
-        f32x4 sacc[4];
+        const bool more = j + kWaves < j1, more2 = j + 2 * kWaves < j1, bad = bad_n;
+        const float ks = pow2_of_byte(ke);
+        f32x4 sacc[TR][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            f32x4 a = {};
+#pragma unroll
+            for (int x = 0; x < TR; ++x) sacc[x][t] = f32x4{};
 #pragma unroll
             for (int k = 0; k < kJ; ++k) {
-                a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(dequant8(kr[t][k][0], kr[t][k][1], ks)),
-                                                            as_bf16x8(qop[2 * k]), a, 0, 0, 0);
-                a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(dequant8(kr[t][k][2], kr[t][k][3], ks)),
-                                                            as_bf16x8(qop[2 * k + 1]), a, 0, 0, 0);
+                const bf16x8 a = as_bf16x8(dequant8(kr[t][k][0], kr[t][k][1], ks)), b8 = as_bf16x8(dequant8(kr[t][k][2], kr[t][k][3], ks));
+#pragma unroll
+                for (int x = 0; x < TR; ++x) {
+                    sacc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(qop[x][2 * k]), sacc[x][t], 0, 0, 0);
+                    sacc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b8, as_bf16x8(qop[x][2 * k + 1]), sacc[x][t], 0, 0, 0);
+                }
             }
-            sacc[t] = a;
         }
-        if (more) load_k(j + kWaves);
+        if (more) {
+            load_k(j + kWaves);
+            if (more2) kpage = look(j + 2 * kWaves, kslot);
+        }
         // Steps that some row does not see whole: scores of hidden keys are
         // -inf, whatever their codes are, and V's codes of keys that no row
         // of the tile sees are zero (what lies behind the last token or in
@@ -213,112 +237,138 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
             __any(bad)) {
             // (bitwise conditions: selects and no branches per score)
             const int k0 = key0 + 16 * grp;
-            const int hi = bad ? -1 : min(pos, s.len - 1) - k0, lo = win_lo - k0, snk = p.sinks - k0;
+            const int snk = p.sinks - k0;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int x = 0; x < TR; ++x) {
+                const int hi = bad ? -1 : min(pos[x], s.len - 1) - k0, lo = p.window > 0 ? pos[x] - p.window + 1 - k0 : -k0;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int k = 4 * t + r;
-                    sacc[t][r] = (k <= hi) & ((k >= lo) | (k < snk)) ? sacc[t][r] : ninf;
-                }
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int k = 4 * t + r;
+                        sacc[x][t][r] = (k <= hi) & ((k >= lo) | (k < snk)) ? sacc[x][t][r] : ninf;
+                    }
+            }
             const uint32_t seen = keys_seen(k0, t_hi, kb.lo, p.sinks, bad);
 #pragma unroll
             for (int t = 0; t < kDT; ++t)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) vr[t][w] &= byte_mask(seen, w);
         }
-        float mx = ninf;
+        u32x4 hi[TR][2], lo[TR][2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int x = 0; x < TR; ++x) {
+            float mx = ninf;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sacc[t][r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = fmaxf(m, mx * p.scale);
-        const float nref = m_new == ninf ? 0.0f : -m_new;
-        const float fac = m == ninf ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
-        if (__any(fac != 1.0f)) {
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int t = 0; t < kDT; ++t)
+                for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sacc[x][t][r]);
+            mx = max_halves(max_quarters(mx));
+            const float m_new = fmaxf(m[x], mx * p.scale);
+            const float nref = m_new == ninf ? 0.0f : -m_new;
+            const float fac = m[x] == ninf ? 1.0f : __builtin_amdgcn_exp2f(m[x] - m_new);
+            if (__any(fac != 1.0f)) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) oacc[t][r] *= fac;
-        }
-        l *= fac;
-        m = m_new;
-        u32x4 hi[2], lo[2];
+                for (int t = 0; t < kDT; ++t)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            float pr[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                pr[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][r], p.scale, nref));
-                l += pr[r];
+                    for (int r = 0; r < 4; ++r) oacc[x][t][r] *= fac;
             }
+            l[x] *= fac;
+            m[x] = m_new;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t w = pack_bf16(pr[2 * e], pr[2 * e + 1]);
-                hi[t >> 1][2 * (t & 1) + e] = w;
-                lo[t >> 1][2 * (t & 1) + e] = pack_bf16(pr[2 * e] - hif8::u2f(w << 16), pr[2 * e + 1] - hif8::u2f(w & 0xffff0000u));
+            for (int t = 0; t < 4; ++t) {
+                float pr[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    pr[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[x][t][r], p.scale, nref));
+                    l[x] += pr[r];
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t w = pack_bf16(pr[2 * e], pr[2 * e + 1]);
+                    hi[x][t >> 1][2 * (t & 1) + e] = w;
+                    lo[x][t >> 1][2 * (t & 1) + e] = pack_bf16(pr[2 * e] - hif8::u2f(w << 16), pr[2 * e + 1] - hif8::u2f(w & 0xffff0000u));
+                }
             }
         }
+        const float vs = pow2_of_byte(ve);
 #pragma unroll
         for (int t = 0; t < kDT; ++t) {
             const bf16x8 v0 = as_bf16x8(dequant8(vr[t][0], vr[t][1], vs)), v1 = as_bf16x8(dequant8(vr[t][2], vr[t][3], vs));
-            oacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, as_bf16x8(hi[0]), oacc[t], 0, 0, 0);
-            oacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, as_bf16x8(hi[1]), oacc[t], 0, 0, 0);
-            oacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, as_bf16x8(lo[0]), oacc[t], 0, 0, 0);
-            oacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, as_bf16x8(lo[1]), oacc[t], 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < TR; ++x) {
+                oacc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, as_bf16x8(hi[x][0]), oacc[x][t], 0, 0, 0);
+                oacc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, as_bf16x8(hi[x][1]), oacc[x][t], 0, 0, 0);
+                oacc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, as_bf16x8(lo[x][0]), oacc[x][t], 0, 0, 0);
+                oacc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, as_bf16x8(lo[x][1]), oacc[x][t], 0, 0, 0);
+            }
         }
-        if (more) load_v(j + kWaves);
+        if (more) {
+            load_v(j + kWaves);
+            if (more2) vpage = look(j + 2 * kWaves, vslot);
+        }
     }
     // the waves' parts: a common maximum, then one sum in a fixed order
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    if (grp == 0) ldm[wave][c16] = m;
-    __syncthreads();
-    float mt = ldm[0][c16];
+    float mt[TR];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) mt = fmaxf(mt, ldm[w][c16]);
-    const float fac = m == ninf ? 0.0f : __builtin_amdgcn_exp2f(m - mt);
-#pragma unroll
-    for (int t = 0; t < kDT; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) oacc[t][r] *= fac;
-    l *= fac;
-    if (grp == 0) ldl[wave][c16] = l;
-    if (wave > 0) {
-#pragma unroll
-        for (int t = 0; t < kDT; ++t) *reinterpret_cast<f32x4*>(&ldo[wave - 1][c16][16 * t + 4 * grp]) = oacc[t];
+    for (int x = 0; x < TR; ++x) {
+        l[x] += __shfl_xor(l[x], 16, 64);
+        l[x] += __shfl_xor(l[x], 32, 64);
+        if (grp == 0) ldm[wave][kRows * x + c16] = m[x];
     }
     __syncthreads();
-    if (wave > 0 || !row_ok) return;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
+    for (int x = 0; x < TR; ++x) {
+        const int r16 = kRows * x + c16;
+        mt[x] = ldm[0][r16];
 #pragma unroll
-        for (int t = 0; t < kDT; ++t) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(&ldo[w - 1][c16][16 * t + 4 * grp]);
+        for (int w = 1; w < kWaves; ++w) mt[x] = fmaxf(mt[x], ldm[w][r16]);
+        const float fac = m[x] == ninf ? 0.0f : __builtin_amdgcn_exp2f(m[x] - mt[x]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) oacc[t][r] += x[r];
+        for (int t = 0; t < kDT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) oacc[x][t][r] *= fac;
+        l[x] *= fac;
+        if (grp == 0) ldl[wave][r16] = l[x];
+        if (wave > 0) {
+#pragma unroll
+            for (int t = 0; t < kDT; ++t) *reinterpret_cast<f32x4*>(&ldo[wave - 1][r16][16 * t + 4 * grp]) = oacc[x][t];
         }
-        l += ldl[w][c16];
     }
-    if (p.nsplit > 1) {
-        const long long at = (long long)split * p.total_q * p.Hq + row;
+    __syncthreads();
+    if (wave > 0) return;
 #pragma unroll
-        for (int t = 0; t < kDT; ++t) *reinterpret_cast<f32x4*>(p.part + at * D + 16 * t + 4 * grp) = oacc[t];
-        if (grp == 0) {
-            p.ml[2 * at] = mt;
-            p.ml[2 * at + 1] = l;
+    for (int x = 0; x < TR; ++x) {
+        if (!row_ok[x]) continue;
+        const int r16 = kRows * x + c16;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+#pragma unroll
+            for (int t = 0; t < kDT; ++t) {
+                const f32x4 y = *reinterpret_cast<const f32x4*>(&ldo[w - 1][r16][16 * t + 4 * grp]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) oacc[x][t][r] += y[r];
+            }
+            l[x] += ldl[w][r16];
         }
-        return;
-    }
-    const bool empty = mt == ninf;
-    const float inv = empty ? 0.0f : 1.0f / l;
+        if (p.nsplit > 1) {
+            const long long at = (long long)split * p.total_q * p.Hq + row[x];
 #pragma unroll
-    for (int t = 0; t < kDT; ++t)
-        *reinterpret_cast<u32x2*>(p.o + row * D + 16 * t + 4 * grp) =
-            u32x2{pack_bf16(oacc[t][0] * inv, oacc[t][1] * inv), pack_bf16(oacc[t][2] * inv, oacc[t][3] * inv)};
-    if (p.lse && grp == 0) p.lse[row] = empty ? ninf : 0.69314718055994531f * (mt + log2f(l));
+            for (int t = 0; t < kDT; ++t) *reinterpret_cast<f32x4*>(p.part + at * D + 16 * t + 4 * grp) = oacc[x][t];
+            if (grp == 0) {
+                p.ml[2 * at] = mt[x];
+                p.ml[2 * at + 1] = l[x];
+            }
+            continue;
+        }
+        const bool empty = mt[x] == ninf;
+        const float inv = empty ? 0.0f : 1.0f / l[x];
+#pragma unroll
+        for (int t = 0; t < kDT; ++t)
+            *reinterpret_cast<u32x2*>(p.o + row[x] * D + 16 * t + 4 * grp) =
+                u32x2{pack_bf16(oacc[x][t][0] * inv, oacc[x][t][1] * inv), pack_bf16(oacc[x][t][2] * inv, oacc[x][t][3] * inv)};
+        if (p.lse && grp == 0) p.lse[row[x]] = empty ? ninf : 0.69314718055994531f * (mt[x] + log2f(l[x]));
+    }
 }
 
 // ---------------------------------------------------------------- tile kernel
@@ -816,48 +866,26 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
 }
 
 // ---------------------------------------------------------------- combine
-// One row per D/4 lanes: the parts' common maximum, then their weighted sums
-// in split order.  Rows that belong to no sequence are left as they are: the
-// row's sequence is looked up, because its parts were not written then.
+// One workgroup per (sequence, row, head); rows that belong to no sequence are
+// none of them and stay as they are.
 template <int D>
 __global__ __launch_bounds__(256) void baps_cache_combine_kernel(CacheAttnParams p)
 {
-    constexpr int kLanes = D / 4, kPer = 256 / kLanes;
-    const long long rows = (long long)p.total_q * p.Hq;
-    const long long row = (long long)blockIdx.x * kPer + threadIdx.x / kLanes;
-    const int d = threadIdx.x % kLanes * 4;
-    if (row >= rows) return;
-    const int t = (int)(row / p.Hq);
-    int lo = 0, hi = p.B;                                       // the last sequence with cu[b] <= t
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.cu[mid] <= t) lo = mid; else hi = mid;
-    }
-    const Seq s = sequence(p, lo);
-    if (t < s.c0 || t >= s.c0 + s.n) return;
-    const float ninf = -__builtin_huge_valf();
-    float m = ninf;
-    for (int k = 0; k < p.nsplit; ++k) m = fmaxf(m, p.ml[2 * (k * rows + row)]);
-    float l = 0.0f;
-    f32x4 o = {};
-    if (m != ninf) {
-        for (int k = 0; k < p.nsplit; ++k) {
-            const float mk = p.ml[2 * (k * rows + row)];
-            if (mk == ninf) continue;
-            const float w = __builtin_amdgcn_exp2f(mk - m);
-            l += w * p.ml[2 * (k * rows + row) + 1];
-            const f32x4 x = *reinterpret_cast<const f32x4*>(p.part + (k * rows + row) * D + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += w * x[e];
-        }
-    }
-    const float inv = m == ninf ? 0.0f : 1.0f / l;
-    *reinterpret_cast<u32x2*>(p.o + row * D + d) = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
-    if (p.lse && d == 0) p.lse[row] = m == ninf ? ninf : 0.69314718055994531f * (m + log2f(l));
+    const int hq = blockIdx.x % p.Hq, i = blockIdx.x / p.Hq % p.max_q, b = blockIdx.x / p.Hq / p.max_q;
+    const Seq s = sequence(p, b);
+    if (i >= s.n) return;
+    const long long row = (long long)(s.c0 + i) * p.Hq + hq;
+    f32x4 o;
+    float lse;
+    if (!combine_row<D>(p.part, p.ml, p.nsplit, (long long)p.total_q * p.Hq, row, o, lse)) return;
+    *reinterpret_cast<u32x2*>(p.o + row * D + 4 * threadIdx.x) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+    if (p.lse && threadIdx.x == 0) p.lse[row] = lse;
 }
 
-// Up to this many flattened rows per key/value head go to the rows kernel
+// Up to this many flattened rows per key/value head go to the rows kernel, 16 or
+// 32 per workgroup
 constexpr long long kFewRows = 64;
+int few_rows_tile(long long flat) { return flat <= kRows ? kRows : 2 * kRows; }
 // Waves of 32 rows in a workgroup of the tile kernel: eight at D = 128, whose
 // tiles' LDS a CU holds once (four, twice: 994 -> 1109 us for 2048 rows on 32768
 // keys, the codes are turned to bf16 twice as often); four at D = 64, two
@@ -870,8 +898,11 @@ hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
 {
     const long long flat = (long long)p.max_q * (p.Hq / p.c.Hkv);
     if (flat <= kFewRows) {
-        const dim3 grid((unsigned)p.nsplit, (unsigned)((flat + kRows - 1) / kRows * p.c.Hkv), (unsigned)p.B);
-        hipLaunchKernelGGL((baps_cache_rows_kernel<D>), grid, dim3(64 * kWaves), 0, st, p);
+        const int rows = few_rows_tile(flat);
+        const dim3 grid((unsigned)p.nsplit, (unsigned)((flat + rows - 1) / rows * p.c.Hkv), (unsigned)p.B), wg(64 * kWaves);
+        if (rows > kRows) hipLaunchKernelGGL((baps_cache_rows_kernel<D, 2, false>), grid, wg, 0, st, p);
+        else if (p.once) hipLaunchKernelGGL((baps_cache_rows_kernel<D, 1, true>), grid, wg, 0, st, p);
+        else hipLaunchKernelGGL((baps_cache_rows_kernel<D, 1, false>), grid, wg, 0, st, p);
     } else {
         static DeviceOnce attr_set;
         const int bytes = 5 * kBlk * D * 2;                     // two blocks of K, three of V
@@ -890,9 +921,7 @@ hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.nsplit == 1) return e;
-    const long long rows = (long long)p.total_q * p.Hq;
-    constexpr int kPer = 256 / (D / 4);
-    hipLaunchKernelGGL((baps_cache_combine_kernel<D>), dim3((unsigned)((rows + kPer - 1) / kPer)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((baps_cache_combine_kernel<D>), dim3((unsigned)((long long)p.B * p.max_q * p.Hq)), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 
@@ -902,7 +931,7 @@ int cache_attention_splits(int B, int Hq, int Hkv, int D, int max_q, int max_len
 {
     const long long flat = (long long)max_q * (Hq / Hkv);
     const bool few = flat <= kFewRows;
-    const int rows = few ? kRows : 32 * (D == 128 ? kTileWaves<128> : kTileWaves<64>);
+    const int rows = few ? few_rows_tile(flat) : 32 * (D == 128 ? kTileWaves<128> : kTileWaves<64>);
     const long long groups = (flat + rows - 1) / rows * Hkv * B;
     long long keys = max_len;                                   // that a workgroup's rows reach
     const long long span = (long long)window + sinks + max_q + 2 * kStep;
@@ -911,7 +940,7 @@ int cache_attention_splits(int B, int Hq, int Hkv, int D, int max_q, int max_len
     const long long slots = few ? 2LL * ncu : ncu, least = few ? 2 * kWaves : 8;    // blocks per split at least
     long long n = slots / groups;
     if (n > blocks / least) n = blocks / least;
-    return (int)(n < 1 ? 1 : (n > 64 ? 64 : n));
+    return (int)(n < 1 ? 1 : (n > kMaxSplits ? kMaxSplits : n));
 }
 
 hipError_t launch_cache_attention(const CacheAttnParams& p, int D, hipStream_t st)
