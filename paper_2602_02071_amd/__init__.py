@@ -343,10 +343,20 @@ def attention_window(q, k, v, window, sinks=0, block=128, lse=True, stream=None,
         raise ValueError("k and v must be [B, Hkv, Sk, D] for q [B, Hq, Sq, D], on one device")
     o = torch.empty((B, Hq, Sq, D), dtype=torch.bfloat16 if out_bf16 else torch.float32, device=q.device)
     l = torch.empty((B, Hq, Sq), dtype=torch.float32, device=q.device) if lse else None
-    with _on_device(q.device):
-        nbytes = baps_attention_window_workspace(B, Hq, Hkv, Sq, Sk, D, window, sinks, block, **knobs)
-        baps_attention_window(q, k, v, o, l, B, Hq, Hkv, Sq, Sk, D, window, sinks, block,
-                              _scratch(nbytes, q.device, stream), nbytes, stream, out_bf16=out_bf16, **knobs)
+    prm = _params(out_bf16=out_bf16, **knobs)
+
+    def run():
+        nbytes = int(load().baps_attention_window_workspace(B, Hq, Hkv, Sq, Sk, D, window, sinks, block, ctypes.byref(prm)))
+        ws = _scratch(nbytes, q.device, stream)
+        _check("baps_attention_window", load().baps_attention_window(
+            _p(q), _p(k), _p(v), _p(o), _p(l), B, Hq, Hkv, Sq, Sk, D, window, sinks, block, ctypes.byref(prm), _p(ws), nbytes,
+            _stream(stream)))
+    guard = _on_device(q.device)
+    if guard is None:
+        run()
+    else:
+        with guard:
+            run()
     return o, l
 
 
@@ -390,10 +400,9 @@ def attention_dump(q, k, v, causal, block, rows, lam=1, n_b0=1, scale_log2=0.0, 
 
 
 def _on_device(device):
-    """A guard that makes `device` the current one (none where it is already)."""
-    import contextlib
+    """A guard that makes `device` the current one (None where it is already)."""
     import torch
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    return None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
 def _scratch(nbytes, device, stream):
@@ -430,6 +439,7 @@ class PagedCache:
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.layers, self.num_pages, self.Hkv, self.page, self.D = layers, pages, Hkv, page, D
         self.device = k.device
+        self._int32, self._bf16, self._float32 = torch.int32, torch.bfloat16, torch.float32
         self.c = baps_cache_t(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), layers, pages, Hkv, page, D)
 
     @classmethod
@@ -439,73 +449,87 @@ class PagedCache:
         return cls(z(layers, num_pages, Hkv, page, D), z(layers, num_pages, Hkv, page // 16, D, 16),
                    z(layers, num_pages, Hkv), z(layers, num_pages, Hkv))
 
-    def _ints(self, **tensors):
-        import torch
-        for name, (t, dim, n) in tensors.items():
-            if t.dtype != torch.int32 or not t.is_contiguous() or t.device != self.device or t.dim() != dim:
-                raise ValueError(f"{name} must be a contiguous int32 tensor of {dim} dimension(s) on {self.device}")
-            if n is not None and t.shape[0] != n:
-                raise ValueError(f"{name} must have {n} rows, not {t.shape[0]}")
+    def _ints(self, name, t, dim, n=None):
+        if t.dtype != self._int32 or not t.is_contiguous() or t.device != self.device or t.dim() != dim:
+            raise ValueError(f"{name} must be a contiguous int32 tensor of {dim} dimension(s) on {self.device}")
+        if n is not None and t.shape[0] != n:
+            raise ValueError(f"{name} must have {n} rows, not {t.shape[0]}")
+
+    def _sequences(self, name, cu, lens, table):
+        """Checks the arrays of a batch; returns its size."""
+        B = lens.shape[0]
+        self._ints("lens", lens, 1)
+        self._ints(name, cu, 1, B + 1)
+        self._ints("table", table, 2, B)
+        return B
 
     def _rows(self, name, t, heads):
         """Packed bf16 rows [T, heads, D], the heads of a row next to each other; returns the row stride."""
-        import torch
-        if (t.dtype != torch.bfloat16 or t.device != self.device or t.dim() != 3 or tuple(t.shape[1:]) != (heads, self.D)
-                or t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.D)):
+        shape, stride = t.shape, t.stride()
+        if (len(shape) != 3 or shape[1] != heads or shape[2] != self.D or t.dtype != self._bf16 or t.device != self.device
+                or stride[2] != 1 or (heads > 1 and stride[1] != self.D)):
             raise ValueError(f"{name} must be bf16 [T, {heads}, {self.D}] on {self.device} with contiguous rows")
-        return t.stride(0) if t.shape[0] > 1 else heads * self.D
+        return stride[0] if shape[0] > 1 else heads * self.D
+
+    def _call(self, fn, *args):
+        guard = _on_device(self.device)
+        if guard is None:
+            return fn(self.c, *args)
+        with guard:
+            return fn(self.c, *args)
 
     def append(self, layer, k, v, cu_new, lens, table, max_new, stream=None):
         """k, v [T, Hkv, D] bf16: the new tokens of every sequence, packed (rows may be strided, both alike)."""
-        B = lens.shape[0]
-        self._ints(cu_new=(cu_new, 1, B + 1), lens=(lens, 1, B), table=(table, 2, B))
+        B = self._sequences("cu_new", cu_new, lens, table)
         stride = self._rows("k", k, self.Hkv)
         if self._rows("v", v, self.Hkv) != stride or k.shape[0] != v.shape[0]:
             raise ValueError("k and v must have the same rows and row stride")
-        with _on_device(self.device):
-            baps_cache_append(self.c, layer, k, v, stride, cu_new, lens, table, table.shape[1], B, k.shape[0], max_new,
-                              stream)
+        self._call(baps_cache_append, layer, k, v, stride, cu_new, lens, table, table.shape[1], B, k.shape[0], max_new, stream)
 
     def attention(self, layer, q, cu_q, lens, table, max_q, max_len, window=0, sinks=0, scale_log2=0.0, lse=True,
                   stream=None):
         """q [T, Hq, D] bf16, packed (rows may be strided); returns o [T, Hq, D] bf16 and lse [T, Hq] (or None)."""
-        import torch
-        B = lens.shape[0]
-        self._ints(cu_q=(cu_q, 1, B + 1), lens=(lens, 1, B), table=(table, 2, B))
+        B = self._sequences("cu_q", cu_q, lens, table)
         T, Hq = q.shape[0], q.shape[1]
         stride = self._rows("q", q, Hq)
-        o = torch.empty((T, Hq, self.D), dtype=torch.bfloat16, device=self.device)
-        l = torch.empty((T, Hq), dtype=torch.float32, device=self.device) if lse else None
-        with _on_device(self.device):
-            nbytes = baps_cache_attention_workspace(self.c, B, Hq, T, max_q, max_len, window, sinks)
-            baps_cache_attention(self.c, layer, q, stride, o, l, cu_q, lens, table, table.shape[1], B, Hq, T, max_q,
-                                 max_len, window, sinks, scale_log2, _scratch(nbytes, self.device, stream), nbytes, stream)
+        o = q.new_empty((T, Hq, self.D))
+        l = q.new_empty((T, Hq), dtype=self._float32) if lse else None
+
+        def run(c):
+            nbytes = baps_cache_attention_workspace(c, B, Hq, T, max_q, max_len, window, sinks)
+            baps_cache_attention(c, layer, q, stride, o, l, cu_q, lens, table, table.shape[1], B, Hq, T, max_q, max_len,
+                                 window, sinks, scale_log2, _scratch(nbytes, self.device, stream), nbytes, stream)
+        self._call(run)
         return o, l
 
     def fork(self, table, lens, refs, parent, grow=None, stream=None):
         """The next set of sequences: (table, lens, refs, missing), new tensors; the pool's copies are made in place."""
-        import torch
-        B_in, width = table.shape
-        B_out = parent.shape[0]
-        self._ints(table=(table, 2, B_in), lens=(lens, 1, B_in), refs=(refs, 1, self.num_pages), parent=(parent, 1, B_out))
+        B_in, B_out = lens.shape[0], parent.shape[0]
+        self._ints("lens", lens, 1)
+        self._ints("table", table, 2, B_in)
+        self._ints("refs", refs, 1, self.num_pages)
+        self._ints("parent", parent, 1)
         if grow is not None:
-            self._ints(grow=(grow, 1, B_out))
-        new = lambda *s: torch.empty(s, dtype=torch.int32, device=self.device)  # noqa: E731
-        out, lens_out, refs_out, missing = new(B_out, width), new(B_out), new(self.num_pages), new(1)
-        with _on_device(self.device):
+            self._ints("grow", grow, 1, B_out)
+        width = table.shape[1]
+        out, lens_out, refs_out, missing = (refs.new_empty(n) for n in ((B_out, width), B_out, self.num_pages, 1))
+
+        def run(c):
             nbytes = baps_cache_pages_workspace(0, B_out)
-            baps_cache_fork(self.c, table, lens, refs, B_in, parent, grow, B_out, width, out, lens_out, refs_out, missing,
+            baps_cache_fork(c, table, lens, refs, B_in, parent, grow, B_out, width, out, lens_out, refs_out, missing,
                             _scratch(nbytes, self.device, stream), nbytes, stream)
+        self._call(run)
         return out, lens_out, refs_out, missing
 
     def compact(self, table, refs, stream=None):
         """(table, refs, remap, live), new tensors; the pool's pages are moved in place."""
-        import torch
-        self._ints(table=(table, 2, None), refs=(refs, 1, self.num_pages))
-        out, refs_out, remap = torch.empty_like(table), torch.empty_like(refs), torch.empty_like(refs)
-        live = torch.empty(1, dtype=torch.int32, device=self.device)
-        with _on_device(self.device):
+        self._ints("table", table, 2)
+        self._ints("refs", refs, 1, self.num_pages)
+        out, refs_out, remap, live = (refs.new_empty(n) for n in (table.shape, self.num_pages, self.num_pages, 1))
+
+        def run(c):
             nbytes = baps_cache_pages_workspace(self.num_pages, 0)
-            baps_cache_compact(self.c, table, table.numel(), refs, out, refs_out, remap, live,
+            baps_cache_compact(c, table, table.numel(), refs, out, refs_out, remap, live,
                                _scratch(nbytes, self.device, stream), nbytes, stream)
+        self._call(run)
         return out, refs_out, remap, live

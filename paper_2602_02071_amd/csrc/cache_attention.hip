@@ -168,10 +168,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
     const int kslot = 16 * (c16 >> 2) >> lp, vslot = 16 * grp >> lp;
     const uint32_t kin = ((16 * (c16 >> 2) & page_mask) + (c16 & 3)) * D + 16 * grp;
     const uint32_t vin = (16 * grp & page_mask) * D + 16 * c16;
-    u32x4 kr[4][kJ], vr[kDT];
-    uint32_t ke = 0, ve = 0;
+    struct Codes {                                              // a step's K or V, and its scale
+        u32x4 w[kDT];                                           // K: [tile t][piece k] at t * kJ + k
+        uint32_t e;
+        bool bad;
+    };
+    static_assert(4 * kJ == kDT, "K and V of a step take the same registers");
     int kpage = 0, vpage = 0;
-    bool bad_n = false;
     auto look = [&](int jj, int slot) { return trow[(uint32_t)min((kb.block(jj) * kStep >> lp) + slot, p.table_width - 1)]; };
     // (a page that is none is read as the last one, and masked)
     auto page_head = [&](int page) { return min((uint32_t)page, (uint32_t)p.c.num_pages - 1u) * (uint32_t)p.c.Hkv + (uint32_t)h; };
@@ -179,37 +182,44 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
         const u32x4* q = reinterpret_cast<const u32x4*>(at);
         return ONCE ? __builtin_nontemporal_load(q) : *q;
     };
-    auto load_k = [&](int jj) {
+    auto load_k = [&](Codes& c, int jj) {
         const uint32_t ph = page_head(kpage);
         const uint8_t* at = p.c.k + (kb.block(jj) * kStep & page_mask) * D + ((uint64_t)ph * page_bytes + kin);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int k = 0; k < kJ; ++k) kr[t][k] = load16(at + 4 * t * D + 64 * k);
-        ke = p.c.ke[ph];
+            for (int k = 0; k < kJ; ++k) c.w[t * kJ + k] = load16(at + 4 * t * D + 64 * k);
+        c.e = p.c.ke[ph];
     };
-    auto load_v = [&](int jj) {
+    auto load_v = [&](Codes& c, int jj) {
         const uint32_t ph = page_head(vpage);
         const uint8_t* at = p.c.v + (kb.block(jj) * kStep & page_mask) * D + ((uint64_t)ph * page_bytes + vin);
 #pragma unroll
-        for (int t = 0; t < kDT; ++t) vr[t] = load16(at + 256 * t);
-        ve = p.c.ve[ph];
-        bad_n = (unsigned)vpage >= (unsigned)p.c.num_pages;
+        for (int t = 0; t < kDT; ++t) c.w[t] = load16(at + 256 * t);
+        c.e = p.c.ve[ph];
+        c.bad = (unsigned)vpage >= (unsigned)p.c.num_pages;
     };
-    if (j < j1) {
-        kpage = look(j, kslot);
-        vpage = look(j, vslot);
-        load_k(j);
-        load_v(j);
-        if (j + kWaves < j1) {
-            kpage = look(j + kWaves, kslot);
-            vpage = look(j + kWaves, vslot);
-        }
-    }
-    for (; j < j1; j += kWaves) {
+    // One step: the next step's K is loaded when K's registers are read and V when
+    // V's are; at D = 64 with one row tile both ahead of this step, into a second
+    // set of registers (64 sequences of 8192 keys: 84 -> 81 us; at D = 128 the
+    // second set is one too many, 154 -> 181 us).
+    constexpr bool kTwo = TR == 1 && D == 64;
+    auto step = [&](Codes& kc, Codes& vc, Codes& kn, Codes& vn) {
         const int key0 = kb.block(j) * kStep;
-        const bool more = j + kWaves < j1, more2 = j + 2 * kWaves < j1, bad = bad_n;
-        const float ks = pow2_of_byte(ke);
+        const bool more = j + kWaves < j1, more2 = j + 2 * kWaves < j1, bad = vc.bad;
+        auto next_k = [&]() {
+            load_k(kTwo ? kn : kc, j + kWaves);
+            if (more2) kpage = look(j + 2 * kWaves, kslot);
+        };
+        auto next_v = [&]() {
+            load_v(kTwo ? vn : vc, j + kWaves);
+            if (more2) vpage = look(j + 2 * kWaves, vslot);
+        };
+        if (kTwo && more) {
+            next_k();
+            next_v();
+        }
+        const float ks = pow2_of_byte(kc.e);
         f32x4 sacc[TR][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -217,7 +227,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
             for (int x = 0; x < TR; ++x) sacc[x][t] = f32x4{};
 #pragma unroll
             for (int k = 0; k < kJ; ++k) {
-                const bf16x8 a = as_bf16x8(dequant8(kr[t][k][0], kr[t][k][1], ks)), b8 = as_bf16x8(dequant8(kr[t][k][2], kr[t][k][3], ks));
+                const bf16x8 a = as_bf16x8(dequant8(kc.w[t * kJ + k][0], kc.w[t * kJ + k][1], ks)),
+                             b8 = as_bf16x8(dequant8(kc.w[t * kJ + k][2], kc.w[t * kJ + k][3], ks));
 #pragma unroll
                 for (int x = 0; x < TR; ++x) {
                     sacc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(qop[x][2 * k]), sacc[x][t], 0, 0, 0);
@@ -225,10 +236,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
                 }
             }
         }
-        if (more) {
-            load_k(j + kWaves);
-            if (more2) kpage = look(j + 2 * kWaves, kslot);
-        }
+        if (!kTwo && more) next_k();
         // Steps that some row does not see whole: scores of hidden keys are
         // -inf, whatever their codes are, and V's codes of keys that no row
         // of the tile sees are zero (what lies behind the last token or in
@@ -253,7 +261,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
 #pragma unroll
             for (int t = 0; t < kDT; ++t)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) vr[t][w] &= byte_mask(seen, w);
+                for (int w = 0; w < 4; ++w) vc.w[t][w] &= byte_mask(seen, w);
         }
         u32x4 hi[TR][2], lo[TR][2];
 #pragma unroll
@@ -291,10 +299,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
                 }
             }
         }
-        const float vs = pow2_of_byte(ve);
+        const float vs = pow2_of_byte(vc.e);
 #pragma unroll
         for (int t = 0; t < kDT; ++t) {
-            const bf16x8 v0 = as_bf16x8(dequant8(vr[t][0], vr[t][1], vs)), v1 = as_bf16x8(dequant8(vr[t][2], vr[t][3], vs));
+            const bf16x8 v0 = as_bf16x8(dequant8(vc.w[t][0], vc.w[t][1], vs)),
+                         v1 = as_bf16x8(dequant8(vc.w[t][2], vc.w[t][3], vs));
 #pragma unroll
             for (int x = 0; x < TR; ++x) {
                 oacc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, as_bf16x8(hi[x][0]), oacc[x][t], 0, 0, 0);
@@ -303,9 +312,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
                 oacc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, as_bf16x8(lo[x][1]), oacc[x][t], 0, 0, 0);
             }
         }
-        if (more) {
-            load_v(j + kWaves);
-            if (more2) vpage = look(j + 2 * kWaves, vslot);
+        if (!kTwo && more) next_v();
+        j += kWaves;
+    };
+    if (j < j1) {
+        Codes ka, va, kb2, vb2;
+        kpage = look(j, kslot);
+        vpage = look(j, vslot);
+        load_k(ka, j);
+        load_v(va, j);
+        if (j + kWaves < j1) {
+            kpage = look(j + kWaves, kslot);
+            vpage = look(j + kWaves, vslot);
+        }
+        while (true) {
+            step(ka, va, kb2, vb2);
+            if (j >= j1) break;
+            if constexpr (kTwo) {
+                step(kb2, vb2, ka, va);
+                if (j >= j1) break;
+            }
         }
     }
     // the waves' parts: a common maximum, then one sum in a fixed order

@@ -44,7 +44,12 @@ __device__ __forceinline__ int block_scan(int v, int* tmp, int* total)
 
 // ---------------------------------------------------------------- fork
 // What child i takes over from its parent and what it needs.
-__device__ __forceinline__ void plan_child(const CacheForkParams& p, int i, bool first)
+struct Child {
+    int len, src, taken, fresh, over;
+};
+
+template <class Refs>
+__device__ __forceinline__ Child plan_child(const CacheForkParams& p, int i, bool first, const Refs& refs)
 {
     const int par = p.parent[i];
     int len = 0, full = 0, copied = 0, src = -1;
@@ -55,7 +60,7 @@ __device__ __forceinline__ void plan_child(const CacheForkParams& p, int i, bool
             // a partly filled last page is written by the next append, so only
             // one sequence may hold it
             const int tail = p.table_in[(long long)par * p.width + full - 1];
-            if (valid_page(tail, p.num_pages) && !(first && p.refs_in[tail] == 1)) {
+            if (valid_page(tail, p.num_pages) && !(first && refs[tail] == 1)) {
                 src = tail;
                 copied = 1;
             }
@@ -63,14 +68,122 @@ __device__ __forceinline__ void plan_child(const CacheForkParams& p, int i, bool
     }
     const long long grow = p.grow ? max(p.grow[i], 0) : 0;
     const long long more = (len + grow + p.page - 1) / p.page;        // pages in all
-    p.lens_out[i] = len;
-    p.src[i] = src;
-    p.dst[i] = -1;
-    p.taken[i] = full - copied;
-    p.fresh[i] = (int)min(more, (long long)p.width) - full + copied;
-    // those past the table's width (held so low that the sum over the children
-    // stays below 2^30)
-    p.over[i] = (int)min(max(more - p.width, 0LL), (1LL << 30) / p.B_out);
+    // (pages past the table's width are held so low that their sum over the
+    // children stays below 2^30)
+    return Child{len, src, full - copied, (int)min(more, (long long)p.width) - full + copied,
+                 (int)min(max(more - p.width, 0LL), (1LL << 30) / p.B_out)};
+}
+
+// The child that the rank-th fresh page goes to: first[c] <= rank < first[c + 1]
+__device__ __forceinline__ int child_of(const int* first, int n, int rank)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= rank) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// The whole bookkeeping in one workgroup, the references and the children's
+// numbers in LDS: one launch in place of three (8 children of 8 sequences, with
+// the copies, 21.1 -> 18.8 us; at 11600 table entries, 192 of 160 sequences, both
+// take 24.5, and more entries are more than one workgroup should walk).
+// kSmallWords: what LDS holds.
+constexpr int kSmallWords = 32768, kSmallEntries = 8192;
+
+bool fork_is_small(const CacheForkParams& p)
+{
+    return (long long)p.num_pages + p.B_in + 5LL * p.B_out + 1 <= kSmallWords &&
+           ((long long)p.B_in + p.B_out) * p.width <= kSmallEntries;
+}
+
+__global__ __launch_bounds__(kScan) void baps_cache_fork_small_kernel(CacheForkParams p)
+{
+    extern __shared__ int words[];
+    __shared__ int tmp[kScan / 64];
+    int* refs = words;                                          // [num_pages]
+    int* first = refs + p.num_pages;                            // [B_in] a parent's first child
+    int* src = first + p.B_in;                                  // [B_out] each
+    int* dst = src + p.B_out;
+    int* taken = dst + p.B_out;
+    int* par = taken + p.B_out;
+    int* fresh = par + p.B_out;                                 // [B_out + 1]
+    const int tid = threadIdx.x;
+    for (int i = tid; i < p.num_pages; i += kScan) refs[i] = p.refs_in[i];
+    for (int i = tid; i < p.B_in; i += kScan) first[i] = 0x7fffffff;
+    __syncthreads();
+    for (int i = tid; i < p.B_out; i += kScan) {
+        par[i] = p.parent[i];
+        if (valid_page(par[i], p.B_in)) atomicMin(first + par[i], i);
+    }
+    __syncthreads();
+    int over = 0, total;
+    for (int i = tid; i < p.B_out; i += kScan) {
+        const Child c = plan_child(p, i, valid_page(par[i], p.B_in) && first[par[i]] == i, refs);
+        p.lens_out[i] = c.len;
+        src[i] = c.src;
+        dst[i] = -1;
+        taken[i] = c.taken;
+        fresh[i] = c.fresh;
+        over += c.over;
+    }
+    __syncthreads();
+    // (kAtOnce entries of a thread are loaded before the first is used)
+    constexpr int kAtOnce = 4;
+    for (int i0 = tid; i0 < p.B_in * p.width; i0 += kAtOnce * kScan) {
+        int page[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) page[u] = i0 + u * kScan < p.B_in * p.width ? p.table_in[i0 + u * kScan] : -1;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (valid_page(page[u], p.num_pages)) atomicSub(refs + page[u], 1);
+    }
+    for (int i0 = tid; i0 < p.B_out * p.width; i0 += kAtOnce * kScan) {
+        int page[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = i0 + u * kScan, r = min(i / p.width, p.B_out - 1), c = i - r * p.width;
+            page[u] = c < taken[r] ? p.table_in[par[r] * p.width + c] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = i0 + u * kScan;
+            if (i >= p.B_out * p.width) break;
+            const bool ok = valid_page(page[u], p.num_pages);
+            if (ok) atomicAdd(refs + page[u], 1);
+            p.table_out[i] = ok ? page[u] : -1;
+        }
+    }
+    // fresh[i] becomes the rank of child i's first fresh page
+    int want = 0;
+    for (int i0 = 0; i0 < p.B_out; i0 += kScan) {
+        const int i = i0 + tid, v = i < p.B_out ? fresh[i] : 0;
+        const int at = block_scan(v, tmp, &total);
+        if (i < p.B_out) fresh[i] = want + at;
+        want += total;
+    }
+    __syncthreads();                                            // references and table rows are whole
+    // every thread ranks the free pages of a run of its own
+    const int run = (p.num_pages + kScan - 1) / kScan, p0 = min(tid * run, p.num_pages), p1 = min(p0 + run, p.num_pages);
+    int n = 0, found;
+    for (int i = p0; i < p1; ++i) n += refs[i] == 0;
+    int rank = block_scan(n, tmp, &found);
+    for (int i = p0; i < p1 && rank < want; ++i) {
+        if (refs[i] != 0) continue;
+        const int c = child_of(fresh, p.B_out, rank), k = rank - fresh[c];
+        p.table_out[c * p.width + taken[c] + k] = i;
+        refs[i] = 1;
+        if (k == 0 && src[c] >= 0) dst[c] = i;
+        ++rank;
+    }
+    block_scan(over, tmp, &total);                              // (its barriers publish refs and dst)
+    if (tid == 0) p.missing[0] = want - min(found, want) + total;
+    for (int i = tid; i < p.num_pages; i += kScan) p.refs_out[i] = refs[i];
+    for (int i = tid; i < p.B_out; i += kScan) {
+        p.src[i] = src[i];
+        p.dst[i] = dst[i];
+    }
 }
 
 __global__ __launch_bounds__(256) void baps_cache_fork_plan_kernel(CacheForkParams p)
@@ -85,7 +198,15 @@ __global__ __launch_bounds__(256) void baps_cache_fork_plan_kernel(CacheForkPara
         for (int k = threadIdx.x; k < i; k += 256) t |= p.parent[k] == par;
         if (t) twin = 1;
         __syncthreads();
-        if (threadIdx.x == 0) plan_child(p, i, !twin);
+        if (threadIdx.x == 0) {
+            const Child c = plan_child(p, i, !twin, p.refs_in);
+            p.lens_out[i] = c.len;
+            p.src[i] = c.src;
+            p.dst[i] = -1;
+            p.taken[i] = c.taken;
+            p.fresh[i] = c.fresh;
+            p.over[i] = c.over;
+        }
     }
     if (p.refs_out != p.refs_in)
         for (long long k = (long long)blockIdx.x * 256 + threadIdx.x; k < p.num_pages; k += (long long)gridDim.x * 256)
@@ -140,11 +261,7 @@ __global__ __launch_bounds__(kScan) void baps_cache_fork_assign_kernel(CacheFork
         const int rank = found + block_scan(is_free ? 1 : 0, tmp, &total);
         found += total;
         if (!is_free || rank >= want) continue;
-        int lo = 0, hi = p.B_out;                               // the child with fresh[lo] <= rank < fresh[lo + 1]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (p.fresh[mid] <= rank) lo = mid; else hi = mid;
-        }
+        const int lo = child_of(p.fresh, p.B_out, rank);
         const int k = rank - p.fresh[lo];
         p.table_out[(long long)lo * p.width + p.taken[lo] + k] = page;
         p.refs_out[page] = 1;
@@ -190,6 +307,8 @@ __global__ __launch_bounds__(256) void baps_cache_fork_copy_kernel(CacheForkPara
 // ---------------------------------------------------------------- compact
 // The n live pages end up on [0, n): the k-th hole below n takes the k-th live
 // page from n up.  Sources lie behind every target, so the moves need no order.
+// (Bound by its barriers: 4 us for 512 pages, 7 for 3000; with the references in
+// LDS and a run of pages per thread it takes the same.)
 __global__ __launch_bounds__(kScan) void baps_cache_compact_plan_kernel(CacheCompactParams p)
 {
     __shared__ int tmp[kScan / 64];
@@ -252,16 +371,30 @@ __global__ __launch_bounds__(256) void baps_cache_compact_move_kernel(CacheCompa
 
 hipError_t launch_cache_fork(const CacheForkParams& p, hipStream_t st)
 {
-    const int copies = p.refs_out != p.refs_in ? (p.num_pages + 1023) / 1024 : 0;
-    const int g = p.B_out > copies ? p.B_out : (copies > 0 ? copies : 1);
-    hipLaunchKernelGGL(baps_cache_fork_plan_kernel, dim3((unsigned)g), dim3(256), 0, st, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (p.B_out + p.B_in > 0) {
-        hipLaunchKernelGGL(baps_cache_fork_refs_kernel, dim3((unsigned)(p.B_out + p.B_in)), dim3(256), 0, st, p);
+    hipError_t e;
+    if (fork_is_small(p)) {
+        static DeviceOnce attr_set;
+        int dev = 0;
+        if ((e = hipGetDevice(&dev)) != hipSuccess) return e;
+        if (!attr_set.is_done(dev)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(&baps_cache_fork_small_kernel),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kSmallWords);
+            if (e != hipSuccess) return e;
+            attr_set.mark(dev);
+        }
+        const int bytes = 4 * (p.num_pages + p.B_in + 5 * p.B_out + 1);
+        hipLaunchKernelGGL(baps_cache_fork_small_kernel, dim3(1), dim3(kScan), bytes, st, p);
+    } else {
+        const int copies = p.refs_out != p.refs_in ? (p.num_pages + 1023) / 1024 : 0;
+        const int g = p.B_out > copies ? p.B_out : (copies > 0 ? copies : 1);
+        hipLaunchKernelGGL(baps_cache_fork_plan_kernel, dim3((unsigned)g), dim3(256), 0, st, p);
         if ((e = hipGetLastError()) != hipSuccess) return e;
+        if (p.B_out + p.B_in > 0) {
+            hipLaunchKernelGGL(baps_cache_fork_refs_kernel, dim3((unsigned)(p.B_out + p.B_in)), dim3(256), 0, st, p);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL(baps_cache_fork_assign_kernel, dim3(1), dim3(kScan), 0, st, p);
     }
-    hipLaunchKernelGGL(baps_cache_fork_assign_kernel, dim3(1), dim3(kScan), 0, st, p);
     if ((e = hipGetLastError()) != hipSuccess || p.B_out == 0 || p.layers == 0) return e;
     hipLaunchKernelGGL(baps_cache_fork_copy_kernel, dim3((unsigned)p.B_out, (unsigned)p.layers, kParts), dim3(256), 0, st, p);
     return hipGetLastError();

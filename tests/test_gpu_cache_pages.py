@@ -77,15 +77,16 @@ def test_fork_runs_out():
     _fork(pool, cache, table, _i(2 ** 31 - 1, -5), refs, _i(0, 1), _i(-3, 1))
 
 
-@pytest.mark.parametrize("seed", range(6))
+@pytest.mark.parametrize("seed", range(10))
 def test_fork_random(seed):
+    """Small batches (one workgroup keeps the books) and, from seed 6 on, wide tables (the grid does)."""
     r = random.Random(seed)
     page, pages = r.choice([16, 64]), r.choice([40, 1100, 2500])
     B = r.choice([3, 17, 60])
     lens = [r.randint(0, 5 * page) for _ in range(B)]
     pool = H.Pool(seed, 1, pages + 6 * B, 1, page, 64)
     cache = pool.to(DEV)
-    table = pool.tables(lens, width=7)
+    table = pool.tables(lens, width=7 if seed < 6 else 3000)
     extra = [r.randrange(pages) for _ in range(r.randint(0, 30))]
     parent = [r.randint(-1, B) for _ in range(r.choice([2, B, 2 * B]))]
     grow = [r.choice([0, 1, page, 3 * page]) for _ in parent]
