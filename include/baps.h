@@ -219,6 +219,8 @@ int baps_attention_fwd_split_noalloc(const void* q, const void* k, const void* v
  * blocks from key 0, so it holds the sinks) with lambda <= 8 and per-row
  * restart, or in the Default setup; bf16 Q/K, ties away from zero; else
  * BAPS_UNSUPPORTED.
+ * The Default setup's kernels have key tiles of their own: block changes no more
+ * than its roundings.
  * workspace: baps_attention_window_workspace(same sizes and knobs) bytes (0
  * unless rows are few in the Default setup, whose keys are then split over
  * workgroups), 256-byte aligned, contents undefined on entry and on return;

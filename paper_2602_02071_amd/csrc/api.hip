@@ -437,25 +437,34 @@ int split_impl(const void* q, const void* k, const void* v, float* o, float* lse
 }
 
 // ---------------------------------------------------------------- windows
-// The splits of a windowed call with few rows (Default setup) and their
-// workspace: about two workgroups per CU, of two key blocks at least each.
+// The splits of a windowed call in the Default setup and their workspace: about two
+// workgroups per CU, with few rows of two key blocks at least each, in the tile
+// kernel, where window_form() wants them, of eight 64-key blocks.
 void window_plan(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks, int block, int mode, int* nsplit,
                  long long* bytes)
 {
     *nsplit = 1;
     *bytes = 0;
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv || block <= 0 || mode != BAPS_MODE_DEFAULT) return;
-    const long long flat = (long long)Sq * (Hq / Hkv);
-    if (flat > kFewFlatRows) return;
     int ncu = 256;                                  // (without a device: an MI355X)
     if (cu_count(&ncu) != hipSuccess) {
         clear_stale_error();
         ncu = 256;
     }
-    long long keys = (long long)window + sinks + Sq + 2 * block;
+    const long long flat = (long long)Sq * (Hq / Hkv);
+    const bool few = flat <= kFewFlatRows;
+    long long rows = 16, keys = (long long)window + sinks + Sq + 2 * block, kblock = block, least = 2, slots = 2LL * ncu;
     if (keys > Sk) keys = Sk;
-    long long n = 2LL * ncu / ((flat + 15) / 16 * Hkv * B);
-    const long long most = (keys + block - 1) / block / 2;
+    if (!few) {
+        const WindowForm f = window_form(D, flat, Hq / Hkv, (long long)Hkv * B, Sk, window, sinks, ncu);
+        if (!f.keys) return;
+        rows = f.rows;
+        keys = f.keys;
+        kblock = 64;
+        least = 8;
+    }
+    long long n = slots / ((flat + rows - 1) / rows * Hkv * B);
+    const long long most = (keys + kblock - 1) / kblock / least;
     if (n > most) n = most;
     *nsplit = (int)(n < 1 ? 1 : (n > 64 ? 64 : n));
     if (*nsplit > 1) *bytes = align256(*nsplit * (long long)B * Hq * Sq * (D + 2) * 4);
@@ -678,6 +687,7 @@ int baps_attention_window(const void* q, const void* k, const void* v, float* o,
         if (kn.mode == BAPS_MODE_EXP2_HIF8 || (kn.mode == BAPS_MODE_E2E_HIF8 && kn.lambda > kCodeMaxLambda) || p.qk_f8 ||
             p.tie_even || p.restart_rows > 1)
             return BAPS_UNSUPPORTED;
+        if (((long long)Sq * (Hq / Hkv) + 15) / 16 * Hkv * B > (1LL << 24)) return BAPS_UNSUPPORTED;
         long long bytes = 0;
         window_plan(B, Hq, Hkv, Sq, Sk, D, window, sinks, block, kn.mode, &p.nsplit, &bytes);
         if (!workspace_ok(workspace, workspace_bytes, bytes)) return BAPS_INVALID_ARGUMENT;

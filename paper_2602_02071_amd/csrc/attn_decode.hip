@@ -651,12 +651,18 @@ hipError_t launch_window_few(const AttnParams& p, hipStream_t st)
 {
     if (p.mode != kModeDefault) return launch_dec<D, BLK, true, kModeE2E | kModeWindow, false, false, false>(p, st);
     const hipError_t e = launch_dec<D, BLK, true, kModeDefault | kModeWindow, false, false, false>(p, st);
-    if (e != hipSuccess || p.nsplit == 1) return e;
-    hipLaunchKernelGGL((baps_attn_window_combine_kernel<D>), dim3((unsigned)((long long)p.B * p.Hq * p.Sq)), dim3(256), 0, st, p);
-    return hipGetLastError();
+    return e != hipSuccess || p.nsplit == 1 ? e : launch_window_combine(p, D, st);
 }
 
 }  // namespace
+
+hipError_t launch_window_combine(const AttnParams& p, int D, hipStream_t st)
+{
+    const dim3 grid((unsigned)((long long)p.B * p.Hq * p.Sq));
+    if (D == 64) hipLaunchKernelGGL((baps_attn_window_combine_kernel<64>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((baps_attn_window_combine_kernel<128>), grid, dim3(256), 0, st, p);
+    return hipGetLastError();
+}
 
 hipError_t launch_attention_window_few(const AttnParams& p, int D, int block, hipStream_t st)
 {

@@ -3,7 +3,9 @@
 // of its rows reach, in ascending order, and masks inside them.  Alg. 1 takes
 // its decisions on the blocks that a row sees, so a block outside its window
 // changes nothing (a fully masked block is a no-op), and the first blocks, which
-// hold the sinks, are B0 as before.
+// hold the sinks, are B0 as before.  The Default setup takes them for short calls
+// only, with 128-key blocks whatever the call's; others go to attn_window_tile.hip.
+// Few rows, of either setup, go to attn_decode.hip.
 #include "attn_fwd.hpp"
 
 namespace baps {
@@ -14,8 +16,19 @@ template <int D, int BLK>
 hipError_t launch_window(const AttnParams& p, hipStream_t st)
 {
     if ((long long)p.Sq * (p.Hq / p.Hkv) <= kFewFlatRows) return launch_attention_window_few(p, D, BLK, st);
-    return p.mode == kModeDefault ? launch_rows<D, BLK, true, kModeDefault | kModeWindow, false, false, false>(p, st)
-                                  : launch_rows<D, BLK, true, kModeE2E | kModeWindow, false, false, false>(p, st);
+    if (p.mode == kModeDefault) {
+        int ncu = 0;
+        const hipError_t e = cu_count(&ncu);
+        if (e != hipSuccess) return e;
+        const WindowForm f = window_form(D, (long long)p.Sq * (p.Hq / p.Hkv), p.Hq / p.Hkv, (long long)p.Hkv * p.B, p.Sk, p.window,
+                                         p.sinks, ncu);
+        if (f.tile) return launch_attention_window_tile(p, D, f.rows, st);
+        constexpr int kDefault = kModeDefault | kModeWindow;
+        if constexpr (D == 128)
+            if (f.rows == 128) return launch_one<D, 128, 8, 2, true, kDefault, false, false, false, false>(p, st);
+        return launch_one<D, 128, 4, 2, true, kDefault, false, false, false, false>(p, st);
+    }
+    return launch_rows<D, BLK, true, kModeE2E | kModeWindow, false, false, false>(p, st);
 }
 
 }  // namespace

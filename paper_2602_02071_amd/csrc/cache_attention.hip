@@ -16,15 +16,13 @@
 
 #include "cache.hpp"
 #include "combine.hpp"
+#include "tile_core.hpp"
 
 namespace baps {
 
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
 typedef __bf16 bf16x2e __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 
 // eight codes (two words) times 2^(e-127), e given as that power's fp32 value
 __device__ __forceinline__ u32x4 dequant8(uint32_t a, uint32_t b, float s)
@@ -36,20 +34,6 @@ __device__ __forceinline__ u32x4 dequant8(uint32_t a, uint32_t b, float s)
 }
 
 __device__ __forceinline__ float pow2_of_byte(int e) { return hif8::u2f((uint32_t)e << 23); }
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
-{
-    const bf16x2 v = {(__bf16)a, (__bf16)b};
-    return __builtin_bit_cast(uint32_t, v);
-}
-
-// the larger of the values of lanes l and l ^ 32
-__device__ __forceinline__ float max_halves(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return fmaxf(hif8::u2f(r[0]), hif8::u2f(r[1]));
-}
 
 // the larger of the values of lanes l and l ^ 16
 __device__ __forceinline__ float max_quarters(float x)
@@ -398,26 +382,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
 }
 
 // ---------------------------------------------------------------- tile kernel
-// NW waves of 32 rows each, blocks of 64 keys.  The codes of a block come
-// through registers (one 16-byte load of K and of V per thread at D = 128),
-// are dequantised once for all waves and stored to LDS as bf16.  K lies as
-// [key][d], V as [d][key], both with their 16-byte chunks XOR-swizzled (reads
-// and stores without bank conflicts).  S^T = K Q^T on 32x32x16 with the rows of
-// K taken in the order that gives a lane 8 consecutive keys per 16-key chunk
-// (row 8a + 4 half + b of 32 is key 16 (a/2) + 8 half + 4 (a%2) + b), so V^T's
-// operand is one 16-byte read and P never leaves its lane.
-//
-// What bounds it: the instructions of a wave.  Per block and wave 32 MFMAs take
-// 1024 cycles of the SIMD, the exponentials with their exponent, sum and packing
-// 740, staging 250, the maxima 160, for two waves per SIMD.  So the two products
-// and the exponentials of neighbouring half blocks are interleaved by hand, one
-// MFMA each (fused); staging has no address arithmetic beyond one 64-bit
-// product; the reference moves by lazy steps.  2048 rows on 32768 keys (GQA
-// 32/8, D = 128): 1207 us in straight order, 1157 interleaved, 1051 with the
-// short staging, 1000 with the wave's priority raised over the products
-// (1.07 PFLOP/s; without staging it would be 908, without the waits for one
-// another 830).
-constexpr int kBlk = 64;
+// NW waves of 32 rows each on the inner loop of tile_core.hpp.  The codes of a
+// block come through registers (one 16-byte load of K and of V per thread at D =
+// 128), are dequantised once for all waves and stored to LDS as bf16; staging has
+// no address arithmetic beyond one 64-bit product, for it is a fifth of a wave's
+// instructions.  2048 rows on 32768 keys (GQA 32/8, D = 128): 1207 us in straight
+// order, 1157 interleaved, 1051 with the short staging, 1000 with the wave's
+// priority raised over the products (1.07 PFLOP/s; without staging it would be
+// 908, without the waits for one another 830).
 
 // sum over the wave's lanes (DPP: no LDS round trips)
 __device__ __forceinline__ int wave_sum_uniform(int v)
@@ -502,9 +474,8 @@ __device__ __forceinline__ TileAt tile_of_rank(const CacheAttnParams& p, int ran
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnParams p)
 {
-    constexpr int kTileRows = 32 * NW;
-    constexpr int kDK = D / 16, kDT = D / 32, kKT = kBlk / 32;
-    constexpr int kKB = kBlk * D * 2;                           // bytes of a K (or V) tile
+    using Core = TileCore<D, false>;
+    constexpr int kTileRows = 32 * NW, kHalf = Core::kHalf, kVBase = Core::kVBase;
     constexpr int kChunks = kBlk * D / 16;                      // 16-byte pieces of codes (512 or 256)
     constexpr int kPer = (kChunks + 64 * NW - 1) / (64 * NW);   // of a thread
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -542,10 +513,11 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
     const int per = (kb.n + p.nsplit - 1) / p.nsplit;
     const int j0 = split * per, j1 = min(kb.n, j0 + per);
 
-    u32x4 qop[kDK];
+    Core core;
+    core.init(lds, lane, p.scale);
 #pragma unroll
-    for (int k = 0; k < kDK; ++k)
-        qop[k] = *reinterpret_cast<const u32x4*>(p.q + (s.c0 + i) * p.qstride + hq * D + 16 * k + 8 * half);
+    for (int k = 0; k < Core::kDK; ++k)
+        core.qop[k] = *reinterpret_cast<const u32x4*>(p.q + (s.c0 + i) * p.qstride + hq * D + 16 * k + 8 * half);
 
     const int* trow = p.table + (long long)b * p.table_width;
     const int lp = p.c.lpage, page_mask = (1 << lp) - 1;
@@ -647,9 +619,6 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
             for (int w = 0; w < 4; ++w) vraw[u][w] &= byte_mask(seen, w);
         }
     };
-    // LDS: four half blocks of K (half 2 j of block j in slot 2 j % 4), then three
-    // blocks of V^T
-    constexpr int kHalf = 32 * 2 * D, kVBase = 4 * kHalf;
     auto store_k = [&](int slot) {                              // the pair into slots slot and (slot + 1) % 4
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
@@ -670,127 +639,19 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
     };
 
     const float ninf = -__builtin_huge_valf();
-    float m = ninf, l = 0.0f, l2 = 0.0f, nref = 0.0f;
-    f32x16 oacc[kDT];
-#pragma unroll
-    for (int t = 0; t < kDT; ++t) oacc[t] = f32x16{};
-    // the lane's K rows: row j32 of a half block is key 16 (a/2) + 8 hf + 4 (a%2) + b
-    const int ka = j32 >> 3, kh = (j32 >> 2) & 1;
-    const int krow = 16 * (ka >> 1) + 8 * kh + 4 * (ka & 1) + (j32 & 3);
-    const int kx = D == 128 ? (krow & 15) : ((krow >> 1) & 7);
-    const int vx = (j32 >> 1) & 7;                              // (the same for j32 + 32 t)
-    uint32_t koff[kDK], voff[2 * kKT];
-#pragma unroll
-    for (int k = 0; k < kDK; ++k) koff[k] = krow * 2 * D + 16 * ((2 * k + half) ^ kx);
-#pragma unroll
-    for (int c = 0; c < 2 * kKT; ++c) voff[c] = j32 * 2 * kBlk + 16 * ((2 * c + half) ^ vx);
-
-    auto k_read = [&](int k, int slot) { return *reinterpret_cast<const u32x4*>(lds + koff[k] + slot * kHalf); };
-    auto v_read = [&](uint32_t at, int dt) { return *reinterpret_cast<const u32x4*>(lds + at + 32 * dt * 2 * kBlk); };
-    // P of the upper 16 of the current 32 keys, and where their V is: their
-    // product is formed beside the next 32 keys' scores
-    u32x4 late = {};
-    uint32_t late_at = kVBase + voff[0];
-    auto finish = [&]() {
-#pragma unroll
-        for (int d = 0; d < kDT; ++d)
-            oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v_read(late_at, d)), as_bf16x8(late), oacc[d], 0, 0, 0);
-        late = u32x4{0, 0, 0, 0};
-    };
-    // masks 32 keys' scores and takes the reference that their P are formed
-    // against.  That is the running maximum only up to a factor of 2^8: it moves
-    // when a row's maximum passes it by more, so that the output is rarely
-    // rescaled (P stays within 2^8 of 1, in floating point at the same relative
-    // precision, and the sums in fp32).
+    // masks 32 keys' scores
     auto settle = [&](f32x16& sc, int key0) {
         if (key0 + 31 > w_lo || (p.window > 0 && key0 <= w_hi - p.window && key0 + 32 > p.sinks) || holes || wf0 + 31 >= flat) {
-            const int k0 = key0 + 8 * half;
+            const int k0 = key0 + Core::kKeyHalf * half;
             const int hi = pos - k0, lo = win_lo - k0, snk = p.sinks - k0;
             const bool gone0 = holes && no_page(page_of(key0)), gone1 = holes && no_page(page_of(key0 + 16));
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int k = 16 * (r >> 3) + (r & 7);
+                const int k = Core::key_of(r);
                 sc[r] = (k <= hi) & ((k >= lo) | (k < snk)) & !(r < 8 ? gone0 : gone1) ? sc[r] : ninf;
             }
         }
-        float mx = ninf;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-        mx = max_halves(mx) * p.scale;
-        if (__any(mx > m + 8.0f)) {                             // (m = -inf: any finite maximum)
-            const float m_new = fmaxf(m, mx);
-            const float fac = m == ninf ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
-            finish();
-#pragma unroll
-            for (int t = 0; t < kDT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) oacc[t][r] *= fac;
-            l *= fac;
-            l2 *= fac;
-            m = m_new;
-            nref = m == ninf ? 0.0f : -m;
-        }
-    };
-    // Q^T of the next 32 keys and P V of the current ones in turn, one MFMA each:
-    // first the late 16 keys of the 32 before, then the current lower 16.  The
-    // current scores turn into P between them, one per MFMA (D = 128), their
-    // exponent, exponential and sum each one MFMA after the other, so that no
-    // instruction waits for the one before it; each operand is read from LDS
-    // kAhead MFMAs before its use.  (The order is written out: left to the
-    // compiler, the reads come one MFMA ahead and the exponentials in a bunch.)
-    auto fused = [&](const f32x16& cur, f32x16& nxt, int slot, int at, int up) {
-        constexpr int kN = 2 * kDK, kAhead = 4, kPerSlot = 16 / kN + (16 % kN ? 1 : 0);
-        static_assert(kDK == 2 * kDT, "as many MFMAs of Q^T as of P V");
-        const uint32_t vlow = at + voff[2 * up];
-        auto operand = [&](int i) {
-            if (i & 1) return k_read(i >> 1, slot);
-            const int n = i >> 1;                               // P V: n < kDT late, then the current lower 16 keys
-            return n < kDT ? v_read(late_at, n) : v_read(vlow, n - kDT);
-        };
-        u32x4 fr[kAhead], pop[2];
-        float x[16];
-        auto stage = [&](int r, int s) {
-            if (r < 0 || r >= 16) return;
-            if (s == 0) x[r] = __builtin_fmaf(cur[r], p.scale, nref);
-            if (s == 1) x[r] = __builtin_amdgcn_exp2f(x[r]);
-            if (s == 2) {
-                if (r & 1) l2 += x[r]; else l += x[r];
-                if (r & 1) pop[r >> 3][(r & 7) >> 1] = pack_bf16(x[r - 1], x[r]);
-            }
-        };
-        constexpr int kLead = 4;                                // scores that are ahead of their MFMA
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) fr[i] = operand(i);
-#pragma unroll
-        for (int r = 0; r < kLead; ++r) stage(r, 0);
-#pragma unroll
-        for (int r = 0; r < kLead - 2; ++r) stage(r, 1);
-#pragma unroll
-        for (int r = 0; r < kLead - 4; ++r) stage(r, 2);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const bf16x8 a = as_bf16x8(fr[i % kAhead]);
-            const int n = i >> 1;
-            if (i & 1) nxt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, as_bf16x8(qop[n]), n ? nxt : f32x16{}, 0, 0, 0);
-            else oacc[n % kDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, as_bf16x8(n < kDT ? late : pop[0]), oacc[n % kDT], 0, 0, 0);
-            if (i + kAhead < kN) fr[i % kAhead] = operand(i + kAhead);
-#pragma unroll
-            for (int e = 0; e < kPerSlot; ++e) {
-                const int r = kPerSlot * i + e;
-                stage(r + kLead, 0);
-                stage(r + kLead - 2, 1);
-                stage(r + kLead - 4, 2);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int r = kPerSlot * kN + kLead - 4; r < 16; ++r) stage(r, 2);
-        late = pop[1];
-        late_at = at + voff[2 * up + 1];
-        // (formed here, not where it is read)
-        asm volatile("" : "+v"(late[0]), "+v"(late[1]), "+v"(late[2]), "+v"(late[3]));
+        core.settle(sc);
     };
 
     // The scores of the next 32 keys are formed while those of the current 32
@@ -798,14 +659,14 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
     // step j LDS holds the halves 2 j + 1 and 2 j + 2 of K and V of blocks j - 1
     // and j; 2 j + 3, 2 j + 4 and V of j + 1 come in.
     f32x16 sa, sb;
-    int vcur = kVBase, vnext = kVBase + kKB;
+    uint32_t vcur = kVBase, vnext = Core::next_v(kVBase);
     auto step = [&](auto par_, int j) {
         constexpr int par = decltype(par_)::value, s1 = 2 * par + 1, s2 = (2 * par + 2) & 3;   // par: (j - j0) & 1
         const bool more = j + 1 < j1;
         __syncthreads();
         if (more) clean_v(j + 1);
         __builtin_amdgcn_s_setprio(1);                          // (the other wave of the SIMD settles meanwhile)
-        fused(sa, sb, s1, vcur, 0);
+        core.fused(sa, sb, s1, vcur, 0);
         __builtin_amdgcn_s_setprio(0);
         settle(sb, kb.block(j) * kBlk + 32);
         if (more) {
@@ -816,7 +677,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
             }
         }
         __builtin_amdgcn_s_setprio(1);
-        fused(sb, sa, s2, vcur, 1);                             // (past the last block: scores that nobody reads)
+        core.fused(sb, sa, s2, vcur, 1);                             // (past the last block: scores that nobody reads)
         __builtin_amdgcn_s_setprio(0);
         if (more) {
             settle(sa, kb.block(j + 1) * kBlk);
@@ -827,7 +688,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
             }
         }
         vcur = vnext;
-        vnext = vnext == kVBase + 2 * kKB ? kVBase : vnext + kKB;
+        vnext = Core::next_v(vnext);
     };
     if (j0 < j1) {
         look_k(j0 - 1);
@@ -851,28 +712,22 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
             if (j0 + 2 < j1) look_k(j0 + 2);
         }
         __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kDK; ++k)
-            sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k_read(k, 0)), as_bf16x8(qop[k]), k ? sa : f32x16{}, 0, 0, 0);
+        core.first(sa, 0);
         settle(sa, kb.block(j0) * kBlk);
         for (int j = j0; j < j1; j += 2) {
             step(std::integral_constant<int, 0>{}, j);
             if (j + 1 < j1) step(std::integral_constant<int, 1>{}, j + 1);
         }
-        finish();
+        core.finish();
     }
-    l += l2;
-    l += __shfl_xor(l, 32, 64);
+    const float l = core.total(), m = core.m;
     if (!row_ok) return;
-    // register r of d tile dt is element 32 dt + 8 (r/4) + 4 half + r%4
     if (p.nsplit > 1) {
         const long long at = (long long)split * p.total_q * p.Hq + row;
 #pragma unroll
-        for (int dt = 0; dt < kDT; ++dt)
+        for (int t = 0; t < Core::kDT; ++t)
 #pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4)
-                *reinterpret_cast<f32x4*>(p.part + at * D + 32 * dt + 8 * q4 + 4 * half) =
-                    f32x4{oacc[dt][4 * q4], oacc[dt][4 * q4 + 1], oacc[dt][4 * q4 + 2], oacc[dt][4 * q4 + 3]};
+            for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4*>(p.part + at * D + 32 * t + 8 * q + 4 * half) = core.out4(t, q, 1.0f);
         if (half == 0) {
             p.ml[2 * at] = m;
             p.ml[2 * at + 1] = l;
@@ -882,12 +737,12 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
     const bool empty = m == ninf;
     const float inv = empty ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (int dt = 0; dt < kDT; ++dt)
+    for (int t = 0; t < Core::kDT; ++t)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
-            *reinterpret_cast<u32x2*>(p.o + row * D + 32 * dt + 8 * q4 + 4 * half) =
-                u32x2{pack_bf16(oacc[dt][4 * q4] * inv, oacc[dt][4 * q4 + 1] * inv),
-                      pack_bf16(oacc[dt][4 * q4 + 2] * inv, oacc[dt][4 * q4 + 3] * inv)};
+        for (int q = 0; q < 4; ++q) {
+            const f32x4 v = core.out4(t, q, inv);
+            *reinterpret_cast<u32x2*>(p.o + row * D + 32 * t + 8 * q + 4 * half) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        }
     if (p.lse && half == 0) p.lse[row] = empty ? ninf : 0.69314718055994531f * (m + log2f(l));
 }
 
@@ -931,7 +786,7 @@ hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
         else hipLaunchKernelGGL((baps_cache_rows_kernel<D, 1, false>), grid, wg, 0, st, p);
     } else {
         static DeviceOnce attr_set;
-        const int bytes = 5 * kBlk * D * 2;                     // two blocks of K, three of V
+        const int bytes = TileCore<D, false>::kLds;
         int dev = 0;
         hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;

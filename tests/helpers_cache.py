@@ -93,24 +93,23 @@ def attend(q, k, v, pos, window, sinks, ok=None, scale=None):
     lse = torch.full((n, Hq), -math.inf, dtype=torch.float64)
     size = torch.zeros((n, Hq), dtype=torch.float64)
     mean = torch.zeros((n, Hq, D), dtype=torch.float64)
-    c = torch.arange(k.shape[1])
-    for i in range(n):
-        t = int(pos[i])
-        seen = c <= t
-        if window:
-            seen &= (c > t - window) | (c < sinks)
-        if ok is not None:
-            seen &= ok
-        if not bool(seen.any()):
-            continue
-        for h in range(Hq):
-            kk, vv = k[h // G][seen], v[h // G][seen]
-            s = kk @ q[i, h].double() * scale
-            size[i, h] = (kk.abs() @ q[i, h].double().abs() * scale).max()
-            lse[i, h] = torch.logsumexp(s, 0)
-            w = torch.exp(s - lse[i, h])
-            o[i, h] = w @ vv
-            mean[i, h] = w @ vv.abs()
+    c, t = torch.arange(k.shape[1]), torch.as_tensor(list(pos), dtype=torch.int64)[:, None]
+    seen = c <= t
+    if window:
+        seen &= (c > t - window) | (c < sinks)
+    if ok is not None:
+        seen &= ok
+    if not n or not len(c):
+        return o, lse, size, mean
+    q = q.double()
+    for h in range(Hq):
+        kk, vv = k[h // G], v[h // G]
+        s = torch.where(seen, q[:, h] @ kk.t() * scale, -math.inf)
+        size[:, h] = torch.where(seen, q[:, h].abs() @ kk.abs().t() * scale, 0).amax(1)
+        lse[:, h] = torch.logsumexp(s, 1)
+        w = torch.exp(s - lse[:, h].where(seen.any(1), torch.zeros(()).double())[:, None])
+        o[:, h] = w @ vv
+        mean[:, h] = w @ vv.abs()
     return o, lse, size, mean
 
 

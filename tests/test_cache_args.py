@@ -47,7 +47,7 @@ def test_window(lib):
     need = baps.baps_attention_window_workspace(1, 4, 2, 1, 9000, 128, 5000, 0, 64, mode=baps.BAPS_MODE_DEFAULT)
     assert need > 0 and need % 256 == 0
     assert call(**long) == BAD and call(**long, ws=A, n=need - 1) == BAD and call(**long, ws=A + 16, n=need) == BAD
-    assert baps.baps_attention_window_workspace(1, 4, 2, 500, 9000, 128, 5000, 0, 64, mode=baps.BAPS_MODE_DEFAULT) == 0
+    assert baps.baps_attention_window_workspace(1, 4, 2, 90000, 90000, 128, 5000, 0, 64, mode=baps.BAPS_MODE_DEFAULT) == 0
     assert baps.baps_attention_window_workspace(1, 4, 2, 1, 9000, 128, 0, 0, 64, mode=baps.BAPS_MODE_DEFAULT) == 0
     assert baps.baps_attention_window_workspace(1, 4, 2, 1, 9000, 128, 5000, 0, 64) == 0
 

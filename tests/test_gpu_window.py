@@ -67,6 +67,25 @@ def test_default_split_keys():
     _default((2, 2, 2, 3, 3000, 64), 2000, 200, 32)
 
 
+@pytest.mark.parametrize("shape", [(1, 4, 2, 100, 2500, 128), (1, 2, 1, 70, 3001, 64), (2, 3, 1, 90, 2200, 128)])
+def test_default_split_keys_many_rows(shape):
+    """Few tiles of many rows over long windows: the keys are split over workgroups."""
+    import paper_2602_02071_amd as baps
+    assert baps.baps_attention_window_workspace(*shape, 2000, 4, 128, mode=DEFAULT) > 0
+    for out_bf16 in (False, True):
+        _default(shape, 2000, 4, 128, out_bf16)
+    _default(shape, 4000, 0, 32)
+    _default(shape, 1700, 70, 64)
+
+
+@pytest.mark.parametrize("shape", [(1, 16, 16, 1100, 1100, 64), (4, 35, 35, 400, 401, 64), (1, 32, 8, 1100, 1100, 128),
+                                   (3, 20, 4, 600, 601, 128), (1, 32, 8, 1500, 1200, 128), (1, 8, 8, 2100, 2100, 128)])
+def test_default_many_items(shape):
+    """More workgroups than CUs, or than 64- or 128-row items would be: the tile kernel, and the forms beside it."""
+    for window, sinks, block in ((100, 0, 64), (333, 5, 128), (1, 1, 32), (64, 65, 64)):
+        _default(shape, window, sinks, block)
+
+
 def test_default_large_scores_and_scale():
     _default((1, 4, 2, 1, 400, 128), 100, 4, 64, q_scale=30.0)
     _default((1, 4, 2, 90, 400, 64), 100, 4, 64, q_scale=30.0)
@@ -154,17 +173,16 @@ def test_alg1_knobs(knobs):
         _alg1(shape, 300, 0, 32, inputs=make_slow_climb(*shape, 0.7, 32), **knobs)
 
 
-@pytest.mark.parametrize("mode", [DEFAULT, E2E])
 @pytest.mark.parametrize("block", [32, 64, 128])
 @pytest.mark.parametrize("shape", [(1, 8, 2, 300, 300, 64), (2, 4, 1, 700, 1000, 128), (1, 32, 8, 1100, 1100, 128), (2, 6, 2, 300, 77, 64)])
-def test_window_of_every_key(shape, block, mode):
-    """A window (or sinks) over all keys is plain causal attention, bit for bit."""
+def test_window_of_every_key(shape, block):
+    """A window (or sinks) over all keys is plain causal attention: Alg. 1 bit for bit (one kernel)."""
     import paper_2602_02071_amd as baps
     B, Hq, Hkv, Sq, Sk, D = shape
     q, k, v = (dev_bf16(x) for x in make_qkv(B, Hq, Hkv, Sq, Sk, D, seed=5, outliers=True))
-    want = baps.attention(q, k, v, True, block, mode=mode)
+    want = baps.attention(q, k, v, True, block)
     for window, sinks in ((Sk, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, Sk)):
-        got = baps.attention_window(q, k, v, window, sinks, block, mode=mode)
+        got = baps.attention_window(q, k, v, window, sinks, block)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (window, sinks)
 
 
