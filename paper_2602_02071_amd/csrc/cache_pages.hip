@@ -74,6 +74,10 @@ __device__ __forceinline__ Child plan_child(const CacheForkParams& p, int i, boo
                  (int)min(max(more - p.width, 0LL), (1LL << 30) / p.B_out)};
 }
 
+// A page that this call copies from is not taken by it, even if nothing holds it
+// any more: between counting and ranking its count reads kRead.
+constexpr int kRead = -0x7fffffff - 1;
+
 // The child that the rank-th fresh page goes to: first[c] <= rank < first[c + 1]
 __device__ __forceinline__ int child_of(const int* first, int n, int rank)
 {
@@ -164,6 +168,9 @@ __global__ __launch_bounds__(kScan) void baps_cache_fork_small_kernel(CacheForkP
         want += total;
     }
     __syncthreads();                                            // references and table rows are whole
+    for (int i = tid; i < p.B_out; i += kScan)
+        if (src[i] >= 0) atomicCAS(refs + src[i], 0, kRead);
+    __syncthreads();
     // every thread ranks the free pages of a run of its own
     const int run = (p.num_pages + kScan - 1) / kScan, p0 = min(tid * run, p.num_pages), p1 = min(p0 + run, p.num_pages);
     int n = 0, found;
@@ -179,7 +186,7 @@ __global__ __launch_bounds__(kScan) void baps_cache_fork_small_kernel(CacheForkP
     }
     block_scan(over, tmp, &total);                              // (its barriers publish refs and dst)
     if (tid == 0) p.missing[0] = want - min(found, want) + total;
-    for (int i = tid; i < p.num_pages; i += kScan) p.refs_out[i] = refs[i];
+    for (int i = tid; i < p.num_pages; i += kScan) p.refs_out[i] = refs[i] == kRead ? 0 : refs[i];
     for (int i = tid; i < p.B_out; i += kScan) {
         p.src[i] = src[i];
         p.dst[i] = dst[i];
@@ -253,6 +260,8 @@ __global__ __launch_bounds__(kScan) void baps_cache_fork_assign_kernel(CacheFork
         want += total;
     }
     if (tid == 0) p.fresh[p.B_out] = want;
+    for (int i = tid; i < p.B_out; i += kScan)
+        if (p.src[i] >= 0) atomicCAS(p.refs_out + p.src[i], 0, kRead);
     __syncthreads();
     int found = 0;
     for (long long p0 = 0; p0 < p.num_pages && found < want; p0 += kScan) {
@@ -267,8 +276,10 @@ __global__ __launch_bounds__(kScan) void baps_cache_fork_assign_kernel(CacheFork
         p.refs_out[page] = 1;
         if (k == 0 && p.src[lo] >= 0) p.dst[lo] = page;
     }
-    block_scan(over, tmp, &total);
+    block_scan(over, tmp, &total);                              // (its barriers end the ranking)
     if (tid == 0) p.missing[0] = want - min(found, want) + total;
+    for (int i = tid; i < p.B_out; i += kScan)
+        if (p.src[i] >= 0) atomicCAS(p.refs_out + p.src[i], kRead, 0);
 }
 
 // ---------------------------------------------------------------- copies

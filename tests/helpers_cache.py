@@ -220,7 +220,7 @@ def fork(page, pages, table, lens, refs, parent, grow):
         out.append(row)
         out_lens.append(n)
         need.append((tail, full, more))
-    free = [at for at in range(pages) if refs[at] == 0]
+    free = [at for at in range(pages) if refs[at] == 0 and at not in {tail for tail, _, _ in need}]
     copies = []
     for i, (tail, full, more) in enumerate(need):
         for c in ([full - 1] if tail is not None else []) + list(range(full, full + more)):

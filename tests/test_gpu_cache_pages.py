@@ -65,6 +65,18 @@ def test_fork_held_elsewhere():
         _fork(pool, cache, table, lens, _refs(8, table, extra), _i(1, 1), _i(64, 0))
 
 
+@pytest.mark.parametrize("width", [2, 3000])
+def test_fork_shared_tails(width):
+    """Rows that share a partly filled page: every child copies it, and it is not taken meanwhile."""
+    pool = H.Pool(4, 2, 12, 2, 16, 128)
+    cache = pool.to(DEV)
+    table = torch.full((4, width), -1, dtype=torch.int32)
+    table[:, :2] = torch.tensor([[5, 1], [4, 1], [3, 2], [6, 2]])
+    for parent in (_i(2, 3, 0, 1), _i(2, 2, 3, 3, 1, 0, 0), _i(3, 0)):
+        _fork(pool, cache, table, _i(20, 25, 17, 31), _refs(12, table), parent, torch.zeros_like(parent))
+        _fork(pool, cache, table, _i(20, 25, 17, 31), _refs(12, table, [1]), parent, None)
+
+
 def test_fork_runs_out():
     """Too few pages, or a table too narrow: counted, -1, and nothing else suffers."""
     pool = H.Pool(3, 2, 6, 1, 16, 64)
