@@ -222,8 +222,8 @@ int baps_attention_fwd_split_noalloc(const void* q, const void* k, const void* v
  * The Default setup's kernels have key tiles of their own: block changes no more
  * than its roundings.
  * workspace: baps_attention_window_workspace(same sizes and knobs) bytes (0
- * unless rows are few in the Default setup, whose keys are then split over
- * workgroups), 256-byte aligned, contents undefined on entry and on return;
+ * unless the keys are split over workgroups, as the Default setup does where
+ * rows are few), 256-byte aligned, contents undefined on entry and on return;
  * calls that may overlap need one each.
  */
 long long baps_attention_window_workspace(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks,
@@ -292,10 +292,10 @@ int baps_get_exp2_lut(unsigned char out_codes[256]);
  *
  * A sequence is a row of a page table, int32 [B][width]: entry j is the page
  * of tokens [j*page, (j+1)*page).  An entry outside [0, num_pages) is "no
- * page": its tokens are not written and count as masked keys.  Lengths beyond
- * width*page (at most 2^30) are taken as width*page.  Tables, lengths, offsets and counts are
- * device arrays, read when the kernels run (a captured call follows their
- * contents).  A page may be in several rows; what is appended to goes to pages
+ * page", as is what lies behind the row: its tokens are not written and count
+ * as masked keys.  width*page is at most 2^30; lengths past 2^30 count as 2^30,
+ * negative ones as 0.  Tables, lengths, offsets and counts are device arrays,
+ * read when the kernels run (a captured call follows their contents).  A page may be in several rows; what is appended to goes to pages
  * that one row holds alone (baps_cache_fork sees to it).
  */
 typedef struct {
@@ -366,7 +366,8 @@ int baps_cache_attention(const baps_cache_t* cache, int layer, const void* q, lo
  *   - every page of the old rows loses one reference, every page of the new
  *     rows has one; pages with none are free, and are taken lowest first, in
  *     the order of the children (a child's copy first, then what it grows by).
- *     Pages given back by this call can be taken by it.
+ *     Pages given back by this call can be taken by it, but for those that it
+ *     copies from.
  * refs_in / refs_out [num_pages] int32: references of every page (callers add
  * their own to hold pages without a row); may be the same array.  table_out
  * [B_out][width], -1 behind the last page; lens_out [B_out].  Neither may

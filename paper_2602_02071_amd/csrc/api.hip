@@ -756,7 +756,7 @@ int baps_cache_attention(const baps_cache_t* cache, int layer, const void* q, lo
     if (!cache_supported(*cache) || !width_ok(*cache, table_width) || B > 65535 || cache->num_pages == 0 || table_width == 0)
         return BAPS_UNSUPPORTED;
     const long long flat = (long long)max_q * (Hq / cache->Hkv);
-    if (flat > (1LL << 30) || 4LL * cache->Hkv > 65535 || (flat + 15) / 16 * B * cache->Hkv > (1LL << 24)) return BAPS_UNSUPPORTED;
+    if (flat > (1LL << 30) || total_q > (1 << 30) || 4LL * cache->Hkv > 65535 || (flat + 15) / 16 * B * cache->Hkv > (1LL << 24)) return BAPS_UNSUPPORTED;
     if (!cache_arrays(*cache) || !q || !o || !cu_q || !lens || !table) return BAPS_INVALID_ARGUMENT;
     if (!aligned16(q) || !aligned16(o) || q_stride < (long long)Hq * cache->D || q_stride % 8) return BAPS_INVALID_ARGUMENT;
     try {
@@ -771,7 +771,8 @@ int baps_cache_attention(const baps_cache_t* cache, int layer, const void* q, lo
         p.lse = lse;
         p.cu = cu_q; p.lens = lens; p.table = table;
         p.table_width = table_width; p.B = B; p.Hq = Hq; p.total_q = total_q; p.max_q = max_q;
-        p.window = window; p.sinks = sinks;
+        p.window = window < (1 << 30) ? window : (1 << 30);        // (no position lies higher, and differences fit an int)
+        p.sinks = sinks;
         p.scale = scale_log2 > 0.0f ? scale_log2 : (float)(1.4426950408889634 / std::sqrt((double)cache->D));
         // K and V that one call streams past the 256 MiB cache in front of memory
         // are read without leaving them there, when one workgroup reads them (64

@@ -74,11 +74,13 @@ __global__ __launch_bounds__((ACfg<D, PAGE>::kThreads)) void baps_cache_append_k
     // every value that comes from the caller's arrays is held to its range
     // before it forms an address
     const int c0 = p.cu[b], c1 = p.cu[b + 1];
+    if (c0 < 0 || c1 <= c0 || c1 > p.total) return;
     const int n = c1 - c0;
     const int len = (int)min((long long)p.lens[b], (long long)p.table_width * PAGE);
+    if (p.lens[b] < n) return;
     const int start = p.lens[b] - n;
-    if (n <= 0 || c0 < 0 || c1 > p.total || start < 0) return;
     const int slot = start / PAGE + blockIdx.x % slots;
+    if (slot >= p.table_width) return;
     const int base = slot * PAGE;
     if (base >= len) return;
     const int page = p.table[(long long)b * p.table_width + slot];

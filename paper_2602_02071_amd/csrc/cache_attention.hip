@@ -51,10 +51,9 @@ struct Seq {
 __device__ __forceinline__ Seq sequence(const CacheAttnParams& p, int b)
 {
     Seq s;
-    const int c1 = p.cu[b + 1], len = min(max(p.lens[b], -(1 << 30)), 1 << 30);
+    const int c1 = p.cu[b + 1], len = min(max(p.lens[b], 0), 1 << 30);
     s.c0 = p.cu[b];
-    s.n = c1 - s.c0;
-    if (s.c0 < 0 || s.n <= 0 || c1 > p.total_q) s.n = 0;
+    s.n = s.c0 < 0 || c1 <= s.c0 || c1 > p.total_q ? 0 : c1 - s.c0;
     s.first = len - s.n;
     s.n = min(s.n, p.max_q);
     s.len = (int)min((long long)len, (long long)p.table_width << p.c.lpage);
@@ -109,7 +108,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
     const int f0 = tile * kTile, flat = s.n * G;
     if (f0 >= flat) return;
 
-    const int t_lo = s.first + f0 / G, t_hi = min(s.first + min(flat - 1, f0 + kTile - 1) / G, s.len - 1);
+    // positions of the workgroup's rows (a window counts from them, also behind the
+    // table's end) and the last key
+    const int t_lo = s.first + f0 / G, p_hi = s.first + min(flat - 1, f0 + kTile - 1) / G, t_hi = min(p_hi, s.len - 1);
     // the lane's rows: c16 of each of the TR row tiles
     bool row_ok[TR];
     int pos[TR];
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
         // -inf, whatever their codes are, and V's codes of keys that no row
         // of the tile sees are zero (what lies behind the last token or in
         // front of the window may be anything, 0 * NaN included).
-        if (key0 + kStep - 1 > t_lo || (p.window > 0 && key0 <= t_hi - p.window && key0 + kStep > p.sinks) ||
+        if (key0 + kStep - 1 > min(t_lo, t_hi) || (p.window > 0 && key0 <= p_hi - p.window && key0 + kStep > p.sinks) ||
             __any(bad)) {
             // (bitwise conditions: selects and no branches per score)
             const int k0 = key0 + 16 * grp;
@@ -428,7 +429,7 @@ __device__ __forceinline__ TileAt tile_of_rank(const CacheAttnParams& p, int ran
     // tiles of a sequence that reach x
     auto reach_of = [&](int len, int n, int x) {
         const int d = len - x;                                  // (no more than 2^30 apart from zero)
-        return d < 0 ? 0 : (int)min((unsigned)n, (unsigned)(((d + 1LL) * G - 1) / R + 1));
+        return d < 0 ? 0 : (int)min((long long)n, ((d + 1LL) * G - 1) / R + 1);
     };
     auto reach = [&](int b, int x) { return b < 64 ? reach_of(len0, tiles0, x) : reach_of(len_of(b), tiles(b), x); };
     auto count = [&](int x) {
@@ -507,7 +508,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
     // positions that the workgroup and this wave hold
     const int t_lo = s.first + f0 / G, t_hi = min(s.first + min(flat - 1, f0 + kTileRows - 1) / G, s.len - 1);
     const int wf0 = f0 + wave * 32;
-    const int w_lo = s.first + wf0 / G, w_hi = min(s.first + min(flat - 1, wf0 + 31) / G, s.len - 1);
+    const int w_lo = min(s.first + wf0 / G, s.len - 1), w_hi = s.first + min(flat - 1, wf0 + 31) / G;
 
     const KeyBlocks kb = key_blocks<kBlk>(t_lo, t_hi, p.window, p.sinks);
     const int per = (kb.n + p.nsplit - 1) / p.nsplit;

@@ -121,6 +121,17 @@ def test_bad_pages_and_rows():
     _same(cache, pool)
 
 
+def test_numbers_near_the_end_of_their_type():
+    pool = H.Pool(8, 1, 5, 1, 16, 64)
+    cache = pool.to(DEV)
+    table = torch.tensor([[0, 1], [2, 3]], dtype=torch.int32)
+    k, v = _new(pool.g, 60, 1, 64), _new(pool.g, 60, 1, 64)
+    top = 2 ** 31 - 1
+    for cu, lens in (([0, 5, 40], [top, 20]), ([0, 40, -top - 1], [20, top]), ([5, -top - 1, 40], [top, 20]), ([top, 5, 9], [top, -top - 1])):
+        _append(pool, cache, 0, k, v, cu, lens, table, 40)
+        _same(cache, pool, f"{cu} {lens}")
+
+
 def test_strided_rows():
     """k and v as slices of one wide projection."""
     pool = H.Pool(6, 1, 8, 2, 16, 64)

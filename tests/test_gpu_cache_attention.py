@@ -116,6 +116,25 @@ def test_longer_than_the_table():
     H.check(o, lse, ref, 32, 64, P_ROWS)
 
 
+@pytest.mark.parametrize("new", [1, 9, 80, 300])
+def test_windows_that_end_behind_the_table(new):
+    """.. whatever the place of the table's end and of the window in a block of keys."""
+    for D, page, width, n in ((64, 16, 5, 200), (128, 16, 9, 150), (128, 64, 2, 190), (64, 128, 1, 1000)):
+        pool = H.Pool(30, 1, 20, 2, page, D)
+        table = pool.tables([width * page, width * page])
+        q = (torch.randn((2 * new, 4, D), generator=pool.g) * 0.4).to(torch.bfloat16)
+        cache = pool.to(DEV)
+        for window, sinks in ((0, 0), (n - 70, 0), (n - 33, 20), (n, 0)):
+            o, lse = cache.attention(0, q.to(DEV), H.ints([0, new, 2 * new], DEV), H.ints([n, n + 13], DEV), table.to(DEV), new,
+                                     n + 13, window, sinks)
+            refs = []
+            for b, m in enumerate((n, n + 13)):
+                k, v, ok = H.sequence_kv(pool, 0, table[b], width * page)
+                refs.append(H.attend(q[b * new:(b + 1) * new], k, v, range(m - new, m), window, sinks))
+            H.check(o, lse, [torch.cat(x) for x in zip(*refs)], n + 13, D, P_ROWS if new * 2 <= 64 else P_TILE,
+                    f"{D} {page} {window} {sinks}")
+
+
 def test_rows_of_nobody_are_left_alone():
     import paper_2602_02071_amd as baps
     for new, fill in (([2, 0, 3], 7.0), ([70, 0, 90], 5.0)):
@@ -155,6 +174,49 @@ def test_offsets_that_make_no_sense():
     # three new tokens of a sequence of one: the first two have no position
     k, v, ok = H.sequence_kv(pool, 0, table[1].cpu(), 1)
     H.check(o[2:5], lse[2:5], H.attend(q[2:5].cpu(), k, v, [-2, -1, 0], 0, 0), 40, 64, P_ROWS)
+
+
+@pytest.mark.parametrize("new,n", [(7, 3), (100, 30), (100, 99)])
+def test_rows_in_front_of_position_zero(new, n):
+    """More new tokens than the sequence is long: the first rows see nothing, whatever the window."""
+    for window in (0, 1, 50, 2 ** 31 - 1):
+        _run(26, [n, 200], [new, 1], 4, 2, 128, 16, window, 0 if not window else 2 ** 31 - 1 - new)
+
+
+@pytest.mark.parametrize("max_q", [3, 100])
+def test_numbers_near_the_end_of_their_type(max_q):
+    """Offsets, lengths, window and sinks at the ends of int32."""
+    import paper_2602_02071_amd as baps
+    top = 2 ** 31 - 1
+    pool = H.Pool(27, 1, 20, 1, 16, 64)
+    cache = pool.to(DEV)
+    table = pool.tables([40, 40, 40]).to(DEV)
+    q = torch.randn((6, 2, 64), generator=pool.g).to(torch.bfloat16).to(DEV)
+    o = torch.full((6, 2, 64), 3.0, dtype=torch.bfloat16, device=DEV)
+    for cu, lens in (([0, 2, -top - 1, 6], [40, top, top]), ([0, 2, top, 0], [40, -top - 1, top])):
+        baps.baps_cache_attention(cache.c, 0, q, 128, o, None, H.ints(cu, DEV), H.ints(lens, DEV), table, table.shape[1], 3, 2, 6,
+                                  max_q, 40, top, top)
+        torch.cuda.synchronize()
+        k, v, ok = H.sequence_kv(pool, 0, table[0].cpu(), 40)
+        ref = H.attend(q[:2].cpu(), k, v, [38, 39], 0, 0)
+        assert (o[:2].cpu().double() - ref[0]).abs().max() < 0.05 * ref[3].max()
+        assert bool((o[2:] == 3.0).all())
+    # a length of 2^31 - 1 counts as 2^30: its row sees all that the table holds
+    o, lse = cache.attention(0, q[:1], H.ints([0, 1], DEV), H.ints([top], DEV), table[:1].contiguous(), max_q, 40, top, top)
+    n = 16 * table.shape[1]
+    k, v, ok = H.sequence_kv(pool, 0, table[0].cpu(), n)
+    H.check(o, lse, H.attend(q[:1].cpu(), k, v, [n - 1], 0, 0, ok), n, 64, P_TILE)
+
+
+@pytest.mark.parametrize("B", [65, 150])
+def test_many_sequences(B):
+    """Chunks of more sequences than a wave has lanes, some of one length, some with nothing."""
+    lens = [(37 * b) % 50 + 1 if b % 7 else 0 for b in range(B)]
+    lens[3] = lens[B - 1] = 170
+    new = [min(n, 5 + 13 * (b % 3)) for b, n in enumerate(lens)]
+    new[3] = new[B - 1] = 90
+    _run(28, lens, new, 4, 2, 64, 16)
+    _run(29, lens, new, 4, 2, 128, 16, 20, 3)
 
 
 def test_strided_rows_and_scale():
