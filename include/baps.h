@@ -220,7 +220,8 @@ int baps_attention_fwd_split_noalloc(const void* q, const void* k, const void* v
  * restart, or in the Default setup; bf16 Q/K, ties away from zero; else
  * BAPS_UNSUPPORTED.
  * The Default setup's kernels have key tiles of their own: block changes no more
- * than its roundings.
+ * than its roundings.  Keys and values that the windows hide from every row may
+ * hold anything; those that some row sees are to be finite.
  * workspace: baps_attention_window_workspace(same sizes and knobs) bytes (0
  * unless the keys are split over workgroups, as the Default setup does where
  * rows are few), 256-byte aligned, contents undefined on entry and on return;

@@ -469,6 +469,10 @@ __global__ __launch_bounds__(64 * (BLK / 32)) void baps_attn_decode_kernel(AttnP
         {
             wait_slot(consumed);
             const char* slot = my_ring + (consumed % RW) * C::kSlotBytes;
+            if (WIN && key0 < kb.lo && key0 + kSlotKeys > p.sinks) {
+                zero_hidden_v<C::kRowBytes>(const_cast<char*>(slot), key0, kSlotKeys, kb.lo, p.sinks, lane, 64);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
 #pragma unroll
             for (int t = 0; t < kDT; ++t) {
                 const char* pa = slot + vrow + 16 * (((16 * t + vd0) >> 3) ^ vx);

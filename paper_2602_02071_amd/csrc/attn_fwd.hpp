@@ -570,6 +570,13 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_fwd_kernel(AttnParams p)
             const char* vt_lds = tiles + (sel * 2 + 1) * C::kTileBytes + kw * kKT * 32 * C::kRowBytes;
             __builtin_amdgcn_s_waitcnt(0);                  // this wave's loads of block jb (and Q) landed
             __syncthreads();                                // everyone's did; block jb-1 fully consumed
+            if constexpr (WIN) {
+                const int lo = cur.tile * C::kTileRows / G + off - p.window + 1;   // the first row's window
+                if (jb * BLK < lo && (jb + 1) * BLK > p.sinks) {
+                    zero_hidden_v<C::kRowBytes>(tiles + (sel * 2 + 1) * C::kTileBytes, jb * BLK, BLK, lo, p.sinks, tid, C::kThreads);
+                    __syncthreads();
+                }
+            }
             // the next block of this item, or the first block of the next
             // item while the last one is computed
             const bool last = jx + 1 == cur.nblk;

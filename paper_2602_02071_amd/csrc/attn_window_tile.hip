@@ -112,7 +112,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_window_tile_kernel(AttnP
     };
 
     const float ninf = -__builtin_huge_valf();
-    auto settle = [&](f32x16& sc, int key0) {
+    auto settle = [&](f32x16& sc, int key0, auto first) {
         if (key0 + 31 > w_lo || (key0 <= w_hi - p.window && key0 + 32 > p.sinks) || wf0 + 31 >= flat) {
             const int k0 = key0 + Core::kKeyHalf * half;
             const int hi = pos - k0, lo = win_lo - k0, snk = p.sinks - k0;
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_window_tile_kernel(AttnP
                 sc[x] = (k <= hi) & ((k >= lo) | (k < snk)) ? sc[x] : ninf;
             }
         }
-        core.settle(sc);
+        core.template settle<decltype(first)::value>(sc);
     };
 
     // In step j LDS holds the halves 2 j + 1 and 2 j + 2 of K and V of blocks j - 1
@@ -132,8 +132,13 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_window_tile_kernel(AttnP
     auto step = [&](auto par_, int j) {
         constexpr int par = decltype(par_)::value, s1 = 2 * par + 1, s2 = (2 * par + 2) & 3;   // par: (j - j0) & 1
         const bool more = j + 1 < j1;
+        const int key0 = kb.block(j) * kBlk;
         __builtin_amdgcn_s_waitcnt(0x0F70);                     // this wave's loads have landed (vmcnt 0)
         __syncthreads();
+        if (key0 < kb.lo && key0 + kBlk > p.sinks) {
+            zero_hidden_v<2 * D>(lds + vcur, key0, kBlk, kb.lo, p.sinks, tid, 64 * NW);
+            __syncthreads();
+        }
         if (more) {
             load_v(j + 1, Core::next_v(vcur));
             load_k(j + 1, (s1 + 2) & 3);
@@ -141,11 +146,11 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_window_tile_kernel(AttnP
         __builtin_amdgcn_s_setprio(1);                          // (the other wave of the SIMD settles meanwhile)
         core.fused(sa, sb, s1, vcur, 0);
         __builtin_amdgcn_s_setprio(0);
-        settle(sb, kb.block(j) * kBlk + 32);
+        settle(sb, key0 + 32, std::false_type{});
         __builtin_amdgcn_s_setprio(1);
         core.fused(sb, sa, s2, vcur, 1);                        // (past the last block: scores that nobody reads)
         __builtin_amdgcn_s_setprio(0);
-        if (more) settle(sa, kb.block(j + 1) * kBlk);
+        if (more) settle(sa, kb.block(j + 1) * kBlk, std::false_type{});
         vcur = Core::next_v(vcur);
     };
     if (j0 < j1) {
@@ -155,7 +160,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_window_tile_kernel(AttnP
         __builtin_amdgcn_s_waitcnt(0x0F70);
         __syncthreads();
         core.first(sa, 0);
-        settle(sa, kb.block(j0) * kBlk);
+        settle(sa, kb.block(j0) * kBlk, std::true_type{});
         for (int j = j0; j < j1; j += 2) {
             step(std::integral_constant<int, 0>{}, j);
             if (j + 1 < j1) step(std::integral_constant<int, 1>{}, j + 1);

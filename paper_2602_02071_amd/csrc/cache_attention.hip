@@ -641,7 +641,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
 
     const float ninf = -__builtin_huge_valf();
     // masks 32 keys' scores
-    auto settle = [&](f32x16& sc, int key0) {
+    auto settle = [&](f32x16& sc, int key0, auto first) {
         if (key0 + 31 > w_lo || (p.window > 0 && key0 <= w_hi - p.window && key0 + 32 > p.sinks) || holes || wf0 + 31 >= flat) {
             const int k0 = key0 + Core::kKeyHalf * half;
             const int hi = pos - k0, lo = win_lo - k0, snk = p.sinks - k0;
@@ -652,7 +652,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
                 sc[r] = (k <= hi) & ((k >= lo) | (k < snk)) & !(r < 8 ? gone0 : gone1) ? sc[r] : ninf;
             }
         }
-        core.settle(sc);
+        core.template settle<decltype(first)::value>(sc);
     };
 
     // The scores of the next 32 keys are formed while those of the current 32
@@ -669,7 +669,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
         __builtin_amdgcn_s_setprio(1);                          // (the other wave of the SIMD settles meanwhile)
         core.fused(sa, sb, s1, vcur, 0);
         __builtin_amdgcn_s_setprio(0);
-        settle(sb, kb.block(j) * kBlk + 32);
+        settle(sb, kb.block(j) * kBlk + 32, std::false_type{});
         if (more) {
             store_v(vnext);
             if (j + 2 < j1) {
@@ -681,7 +681,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
         core.fused(sb, sa, s2, vcur, 1);                             // (past the last block: scores that nobody reads)
         __builtin_amdgcn_s_setprio(0);
         if (more) {
-            settle(sa, kb.block(j + 1) * kBlk);
+            settle(sa, kb.block(j + 1) * kBlk, std::false_type{});
             store_k((s1 + 2) & 3);
             if (j + 2 < j1) {
                 fetch_k(j + 2);
@@ -714,7 +714,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
         }
         __syncthreads();
         core.first(sa, 0);
-        settle(sa, kb.block(j0) * kBlk);
+        settle(sa, kb.block(j0) * kBlk, std::true_type{});
         for (int j = j0; j < j1; j += 2) {
             step(std::integral_constant<int, 0>{}, j);
             if (j + 1 < j1) step(std::integral_constant<int, 1>{}, j + 1);

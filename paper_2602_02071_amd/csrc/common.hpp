@@ -167,6 +167,18 @@ __device__ __forceinline__ KeyBlocks key_blocks(int t_lo, int t_hi, int window, 
     return r;
 }
 
+// Zeros over the rows of an LDS block of V (n keys from key0 on, ROW_BYTES each)
+// that are no sinks and lie in front of lo: nobody's window holds them, their
+// weights are zero, and they may be anything, NaN included.  By `threads`
+// threads, of which this is number t.
+template <int ROW_BYTES>
+__device__ __forceinline__ void zero_hidden_v(char* v, int key0, int n, int lo, int sinks, int t, int threads)
+{
+    const int r1 = min(lo - key0, n);
+    for (int i = max(sinks - key0, 0) * (ROW_BYTES / 16) + t; i < r1 * (ROW_BYTES / 16); i += threads)
+        *reinterpret_cast<u32x4*>(v + 16 * i) = u32x4{0, 0, 0, 0};
+}
+
 struct SoftmaxBlockParams {
     const float* s;
     long long rows, cols, ld;

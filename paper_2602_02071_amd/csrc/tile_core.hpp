@@ -144,7 +144,8 @@ struct TileCore {
     // running maximum only up to a factor of 2^8: it moves when a row's maximum
     // passes it by more, so that the output is rarely rescaled (P stays within 2^8
     // of 1, in floating point at the same relative precision, and the sums in
-    // fp32).
+    // fp32).  FIRST: of the first 32 keys, with nothing summed yet.
+    template <bool FIRST>
     __device__ __forceinline__ void settle(const f32x16& sc)
     {
         const float ninf = -__builtin_huge_valf();
@@ -155,13 +156,15 @@ struct TileCore {
         if (__any(mx > m + 8.0f)) {                             // (m = -inf: any finite maximum)
             const float m_new = fmaxf(m, mx);
             const float fac = m == ninf ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
-            finish();
+            if constexpr (!FIRST) {
+                finish();
 #pragma unroll
-            for (int t = 0; t < kDT; ++t)
+                for (int t = 0; t < kDT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) oacc[t][r] *= fac;
-            l *= fac;
-            l2 *= fac;
+                    for (int r = 0; r < 16; ++r) oacc[t][r] *= fac;
+                l *= fac;
+                l2 *= fac;
+            }
             m = m_new;
             nref = m == ninf ? 0.0f : -m;
         }

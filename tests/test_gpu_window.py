@@ -56,6 +56,27 @@ def test_default_shapes(shape):
         _default(shape, window, sinks, 64, out_bf16=True)
 
 
+@pytest.mark.parametrize("mode", [DEFAULT, E2E])
+@pytest.mark.parametrize("shape", [(2, 8, 2, 1, 700, 128), (1, 4, 1, 13, 333, 64), (1, 4, 2, 203, 601, 128), (1, 2, 2, 130, 900, 64),
+                                   (1, 2, 1, 100, 2500, 128), (1, 32, 32, 600, 1100, 128), (4, 35, 35, 400, 701, 64)])
+def test_hidden_keys_may_be_anything(shape, mode):
+    """NaN and infinities where the windows of all rows end, between them and the sinks: the bits are those of zeros there."""
+    import paper_2602_02071_amd as baps
+    B, Hq, Hkv, Sq, Sk, D = shape
+    q, k, v = (dev_bf16(x) for x in make_qkv(B, Hq, Hkv, Sq, Sk, D, seed=3))
+    for window, sinks, block in ((1, 0, 64), (77, 3, 128), (200, 70, 32), (min(1900, Sk - Sq - 1), 0, 64)):
+        got = []
+        for fill in (0.0, math.nan, math.inf):
+            kk, vv = k.clone(), v.clone()
+            kk[:, :, sinks:max(Sk - Sq - window + 1, sinks)] = fill
+            vv[:, :, sinks:max(Sk - Sq - window + 1, sinks)] = -fill
+            got.append(baps.attention_window(q, kk, vv, window, sinks, block, mode=mode))
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(got[0][0]).all())
+        for o, lse in got[1:]:
+            assert torch.equal(o, got[0][0]) and torch.equal(lse, got[0][1]), f"{shape} {window} {sinks} {block}"
+
+
 def test_default_split_keys():
     """Few streams and a long window: the keys are split over workgroups."""
     import paper_2602_02071_amd as baps
