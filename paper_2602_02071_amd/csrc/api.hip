@@ -516,7 +516,7 @@ int cache_plan(const baps_cache_t& c, int B, int Hq, int total_q, int max_q, int
         clear_stale_error();
         ncu = 256;
     }
-    *nsplit = cache_attention_splits(B, Hq, c.Hkv, c.D, max_q, max_len, window, sinks, ncu);
+    *nsplit = cache_attention_splits(B, Hq, c.Hkv, c.D, total_q, max_q, max_len, window, sinks, ncu);
     if (*nsplit > 1) *bytes = align256((long long)*nsplit * total_q * Hq * (c.D + 2) * 4);
     return BAPS_OK;
 }

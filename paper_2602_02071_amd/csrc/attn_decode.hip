@@ -631,15 +631,9 @@ hipError_t launch_attention_decode(const AttnParams& p, int D, int block, hipStr
 
 namespace {
 
-// One workgroup per row.
 template <int D>
-__global__ __launch_bounds__(256) void baps_attn_window_combine_kernel(AttnParams p)
+__device__ __forceinline__ void store_joined(const AttnParams& p, long long row, int d, f32x4 o, float lse)
 {
-    const long long row = blockIdx.x;
-    f32x4 o;
-    float lse;
-    if (!combine_row<D>(p.part, p.ml, p.nsplit, (long long)p.B * p.Hq * p.Sq, row, o, lse)) return;
-    const int d = 4 * threadIdx.x;
     if (p.out_bf16) {
         const bf16x2 lo = {(__bf16)o[0], (__bf16)o[1]}, hi = {(__bf16)o[2], (__bf16)o[3]};
         *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(p.o) + row * D + d) =
@@ -648,6 +642,41 @@ __global__ __launch_bounds__(256) void baps_attn_window_combine_kernel(AttnParam
         *reinterpret_cast<f32x4*>(p.o + row * D + d) = o;
     }
     if (p.lse && d == 0) p.lse[row] = lse;
+}
+
+// One workgroup per row.
+template <int D>
+__global__ __launch_bounds__(256) void baps_attn_window_combine_kernel(AttnParams p)
+{
+    const long long row = blockIdx.x;
+    f32x4 o;
+    float lse;
+    if (!combine_row<D>(p.part, p.ml, p.nsplit, (long long)p.B * p.Hq * p.Sq, row, o, lse)) return;
+    store_joined<D>(p, row, 4 * threadIdx.x, o, lse);
+}
+
+// Up to kFewSplits parts: 1024 / D rows per workgroup.
+template <int D>
+__global__ __launch_bounds__(256) void baps_attn_window_combine_few_kernel(AttnParams p)
+{
+    const long long rows = (long long)p.B * p.Hq * p.Sq, row = (long long)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
+    const int d4 = threadIdx.x % (D / 4);
+    if (row >= rows) return;
+    f32x4 o;
+    float lse;
+    combine_row_few<D>(p.part, p.ml, p.nsplit, rows, row, d4, o, lse);
+    store_joined<D>(p, row, 4 * d4, o, lse);
+}
+
+template <int D>
+hipError_t launch_combine(const AttnParams& p, hipStream_t st)
+{
+    const long long rows = (long long)p.B * p.Hq * p.Sq;
+    if (p.nsplit <= kFewSplits)
+        hipLaunchKernelGGL((baps_attn_window_combine_few_kernel<D>), dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, p);
+    else
+        hipLaunchKernelGGL((baps_attn_window_combine_kernel<D>), dim3((unsigned)rows), dim3(256), 0, st, p);
+    return hipGetLastError();
 }
 
 template <int D, int BLK>
@@ -662,10 +691,7 @@ hipError_t launch_window_few(const AttnParams& p, hipStream_t st)
 
 hipError_t launch_window_combine(const AttnParams& p, int D, hipStream_t st)
 {
-    const dim3 grid((unsigned)((long long)p.B * p.Hq * p.Sq));
-    if (D == 64) hipLaunchKernelGGL((baps_attn_window_combine_kernel<64>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((baps_attn_window_combine_kernel<128>), grid, dim3(256), 0, st, p);
-    return hipGetLastError();
+    return D == 64 ? launch_combine<64>(p, st) : launch_combine<128>(p, st);
 }
 
 hipError_t launch_attention_window_few(const AttnParams& p, int D, int block, hipStream_t st)

@@ -60,10 +60,11 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_window_tile_kernel(AttnP
     const int split = blockIdx.x / heads % p.nsplit;
     const int f0 = ((flat + kTileRows - 1) / kTileRows - 1 - blockIdx.x / heads / p.nsplit) * kTileRows;
 
-    const int wf0 = f0 + wave * 32, f = wf0 + j32;
-    const bool row_ok = f < flat;
-    const int r = (row_ok ? f : f0) / G, hq = h * G + (row_ok ? f : f0) % G;
-    const int pos = row_ok ? r + off : -1, win_lo = pos - p.window + 1;
+    // (lanes behind the last row compute it again, and store nothing)
+    const int wf0 = min(f0 + wave * 32, flat - 1), f = min(f0 + wave * 32 + j32, flat - 1);
+    const bool row_ok = f0 + wave * 32 + j32 < flat;
+    const int r = f / G, hq = h * G + f % G;
+    const int pos = r + off, win_lo = pos - p.window + 1;
     const long long row = ((long long)b * p.Hq + hq) * p.Sq + r;
     const int t_lo = f0 / G + off, t_hi = min(flat - 1, f0 + kTileRows - 1) / G + off;
     const int w_lo = wf0 / G + off, w_hi = min(flat - 1, wf0 + 31) / G + off;
@@ -113,7 +114,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_attn_window_tile_kernel(AttnP
 
     const float ninf = -__builtin_huge_valf();
     auto settle = [&](f32x16& sc, int key0, auto first) {
-        if (key0 + 31 > w_lo || (key0 <= w_hi - p.window && key0 + 32 > p.sinks) || wf0 + 31 >= flat) {
+        if (key0 + 31 > w_lo || (key0 <= w_hi - p.window && key0 + 32 > p.sinks)) {
             const int k0 = key0 + Core::kKeyHalf * half;
             const int hi = pos - k0, lo = win_lo - k0, snk = p.sinks - k0;
 #pragma unroll

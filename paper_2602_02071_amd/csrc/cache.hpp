@@ -78,6 +78,7 @@ hipError_t launch_cache_compact(const CacheCompactParams& p, hipStream_t st);
 
 // The split of the attention call: how many key splits, for how many keys at
 // most that a row reaches
-int cache_attention_splits(int B, int Hq, int Hkv, int D, int max_q, int max_len, int window, int sinks, int ncu);
+int cache_attention_splits(int B, int Hq, int Hkv, int D, int total_q, int max_q, int max_len, int window, int sinks,
+                           int ncu);
 
 }  // namespace baps

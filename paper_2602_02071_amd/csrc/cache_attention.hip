@@ -12,6 +12,7 @@
 // bytes.  tile: 256 rows per workgroup, for chunks of a prompt; bound by the
 // matrix unit and the exponentials.  Either splits the keys of a row over
 // workgroups where rows alone are too few, and combine joins the parts.
+#include <algorithm>
 #include <type_traits>
 
 #include "cache.hpp"
@@ -499,15 +500,16 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
     if (tile < 0) return;                                       // (the caller's arrays changed meanwhile)
     const int f0 = tile * kTileRows;
 
-    const int f = f0 + wave * 32 + j32;
-    const bool row_ok = f < flat;
-    const int i = (row_ok ? f : f0) / G, hq = h * G + (row_ok ? f : f0) % G;
-    const int pos = row_ok ? min(s.first + i, s.len - 1) : -1;
-    const int win_lo = (row_ok && p.window > 0) ? s.first + i - p.window + 1 : 0;
+    // lanes behind the last row compute it again, and store nothing: no mask for
+    // them in the loop (500 tokens on 3800 keys, D = 64: 64 -> 47 us)
+    const int wf0 = min(f0 + wave * 32, flat - 1);
+    const bool row_ok = f0 + wave * 32 + j32 < flat;
+    const int f = min(f0 + wave * 32 + j32, flat - 1), i = f / G, hq = h * G + f % G;
+    const int pos = min(s.first + i, s.len - 1);
+    const int win_lo = p.window > 0 ? s.first + i - p.window + 1 : 0;
     const long long row = (long long)(s.c0 + i) * p.Hq + hq;
     // positions that the workgroup and this wave hold
     const int t_lo = s.first + f0 / G, t_hi = min(s.first + min(flat - 1, f0 + kTileRows - 1) / G, s.len - 1);
-    const int wf0 = f0 + wave * 32;
     const int w_lo = min(s.first + wf0 / G, s.len - 1), w_hi = s.first + min(flat - 1, wf0 + 31) / G;
 
     const KeyBlocks kb = key_blocks<kBlk>(t_lo, t_hi, p.window, p.sinks);
@@ -642,7 +644,7 @@ __global__ __launch_bounds__(64 * NW, 2) void baps_cache_tile_kernel(CacheAttnPa
     const float ninf = -__builtin_huge_valf();
     // masks 32 keys' scores
     auto settle = [&](f32x16& sc, int key0, auto first) {
-        if (key0 + 31 > w_lo || (p.window > 0 && key0 <= w_hi - p.window && key0 + 32 > p.sinks) || holes || wf0 + 31 >= flat) {
+        if (key0 + 31 > w_lo || (p.window > 0 && key0 <= w_hi - p.window && key0 + 32 > p.sinks) || holes) {
             const int k0 = key0 + Core::kKeyHalf * half;
             const int hi = pos - k0, lo = win_lo - k0, snk = p.sinks - k0;
             const bool gone0 = holes && no_page(page_of(key0)), gone1 = holes && no_page(page_of(key0 + 16));
@@ -764,6 +766,24 @@ __global__ __launch_bounds__(256) void baps_cache_combine_kernel(CacheAttnParams
     if (p.lse && threadIdx.x == 0) p.lse[row] = lse;
 }
 
+// The same for up to kFewSplits parts, 1024 / D rows per workgroup.
+template <int D>
+__global__ __launch_bounds__(256) void baps_cache_combine_few_kernel(CacheAttnParams p)
+{
+    const long long at = (long long)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
+    const int d4 = threadIdx.x % (D / 4);
+    const int hq = (int)(at % p.Hq), i = (int)(at / p.Hq % p.max_q), b = (int)(at / p.Hq / p.max_q);
+    if (b >= p.B) return;
+    const Seq s = sequence(p, b);
+    if (i >= s.n) return;
+    const long long row = (long long)(s.c0 + i) * p.Hq + hq;
+    f32x4 o;
+    float lse;
+    combine_row_few<D>(p.part, p.ml, p.nsplit, (long long)p.total_q * p.Hq, row, d4, o, lse);
+    *reinterpret_cast<u32x2*>(p.o + row * D + 4 * d4) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+    if (p.lse && d4 == 0) p.lse[row] = lse;
+}
+
 // Up to this many flattened rows per key/value head go to the rows kernel, 16 or
 // 32 per workgroup
 constexpr long long kFewRows = 64;
@@ -803,26 +823,57 @@ hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.nsplit == 1) return e;
-    hipLaunchKernelGGL((baps_cache_combine_kernel<D>), dim3((unsigned)((long long)p.B * p.max_q * p.Hq)), dim3(256), 0, st, p);
+    const long long rows = (long long)p.B * p.max_q * p.Hq;
+    if (p.nsplit <= kFewSplits)
+        hipLaunchKernelGGL((baps_cache_combine_few_kernel<D>), dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, p);
+    else
+        hipLaunchKernelGGL((baps_cache_combine_kernel<D>), dim3((unsigned)rows), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int cache_attention_splits(int B, int Hq, int Hkv, int D, int max_q, int max_len, int window, int sinks, int ncu)
+// The time of n splits of the tile kernel's keys, in us beyond what any call takes:
+// the 64-key blocks of a workgroup in turn, or all of them over the workgroups that
+// run at once, and the join: a launch, and the parts written and read.  avg: blocks
+// per tile over a chunk, whose first rows see fewer.  (1024 keys, 256 new: 28 us with
+// two splits, 22 with four, 20 with eight; 32 heads over 8 of 3800, 1850 new, D =
+// 128: 115 whole, 121 with two; 32 over 8 of 9000, 512 new, D = 64: 94 with two, 67
+// with four, 64 with six.)
+double tile_time(int n, int D, double blocks, double avg, double groups, double rows, int ncu)
+{
+    const double step = D == 128 ? 2.0 : 1.4, at_once = D == 128 ? ncu : 2.0 * ncu;
+    const double longest = blocks / n, shared = groups * avg / at_once;
+    return step * (longest > shared ? longest : shared) + (n > 1 ? 6.0 + rows * n * 8 * D / 5e6 : 0.0);
+}
+
+int cache_attention_splits(int B, int Hq, int Hkv, int D, int total_q, int max_q, int max_len, int window, int sinks, int ncu)
 {
     const long long flat = (long long)max_q * (Hq / Hkv);
     const bool few = flat <= kFewRows;
     const int rows = few ? few_rows_tile(flat) : 32 * (D == 128 ? kTileWaves<128> : kTileWaves<64>);
-    const long long groups = (flat + rows - 1) / rows * Hkv * B;
+    // (ragged chunks: no more tiles than all rows fill, and one more each)
+    const long long groups = Hkv * std::min((flat + rows - 1) / rows * B, (long long)total_q * (Hq / Hkv) / rows + B);
     long long keys = max_len;                                   // that a workgroup's rows reach
-    const long long span = (long long)window + sinks + max_q + 2 * kStep;
+    const long long held = few ? max_q : rows / (Hq / Hkv) + 1, span = (long long)window + sinks + held + 2 * kStep;
     if (window > 0 && span < keys) keys = span;
     const long long blocks = (keys + kStep - 1) / kStep;
-    const long long slots = few ? 2LL * ncu : ncu, least = few ? 2 * kWaves : 8;    // blocks per split at least
-    long long n = slots / groups;
-    if (n > blocks / least) n = blocks / least;
-    return (int)(n < 1 ? 1 : (n > kMaxSplits ? kMaxSplits : n));
+    if (few) {
+        const long long n = std::min(2LL * ncu / groups, blocks / (2 * kWaves));    // two waves' blocks per split at least
+        return (int)std::min(std::max(n, 1LL), (long long)kMaxSplits);
+    }
+    const double avg = window > 0 ? (double)blocks : std::max((double)blocks - max_q / 128.0, blocks / 2.0);
+    const double whole = tile_time(1, D, blocks, avg, groups, (double)total_q * Hq, ncu);
+    int best = 1;
+    double least = 0.9 * whole;                                 // (a split is to gain a tenth)
+    for (int n = 2; n <= kMaxSplits && n <= blocks; ++n) {
+        const double t = tile_time(n, D, blocks, avg, groups, (double)total_q * Hq, ncu);
+        if (t < least) {
+            least = t;
+            best = n;
+        }
+    }
+    return best;
 }
 
 hipError_t launch_cache_attention(const CacheAttnParams& p, int D, hipStream_t st)

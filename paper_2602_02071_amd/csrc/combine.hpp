@@ -61,4 +61,48 @@ __device__ __forceinline__ bool combine_row(const float* part, const float* ml, 
     return true;
 }
 
+// Up to kFewSplits parts: D/4 threads per row, d4 of 0 .. D/4 - 1, with all parts'
+// loads in flight at once; several rows per workgroup, for a workgroup per row
+// costs more to start than such a row takes (32768 rows of two parts, D = 128: 32
+// -> 10 us).
+constexpr int kFewSplits = 8;
+
+template <int D>
+__device__ __forceinline__ void combine_row_few(const float* part, const float* ml, int nsplit, long long rows, long long row,
+                                                int d4, f32x4& o, float& lse)
+{
+    const float ninf = -__builtin_huge_valf();
+    float m[kFewSplits], l[kFewSplits];
+    f32x4 x[kFewSplits];
+#pragma unroll
+    for (int k = 0; k < kFewSplits; ++k) {
+        m[k] = ninf;
+        l[k] = 0.0f;
+        x[k] = f32x4{};
+        if (k < nsplit) {
+            const long long at = k * rows + row;
+            m[k] = ml[2 * at];
+            l[k] = ml[2 * at + 1];
+            x[k] = *reinterpret_cast<const f32x4*>(part + at * D + 4 * d4);
+        }
+    }
+    float top = m[0];
+#pragma unroll
+    for (int k = 1; k < kFewSplits; ++k) top = fmaxf(top, m[k]);
+    float total = 0.0f;
+    o = f32x4{};
+#pragma unroll
+    for (int k = 0; k < kFewSplits; ++k) {
+        const float w = m[k] == ninf ? 0.0f : __builtin_amdgcn_exp2f(m[k] - top);
+        total += w * l[k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += w * x[k][e];
+    }
+    const bool empty = top == ninf;
+    const float inv = empty ? 0.0f : 1.0f / total;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= inv;
+    lse = empty ? ninf : 0.69314718055994531f * (top + log2f(total));
+}
+
 }  // namespace baps

@@ -292,17 +292,16 @@ hipError_t launch_attention_window_tile(const AttnParams& p, int D, int rows, hi
 hipError_t launch_window_combine(const AttnParams& p, int D, hipStream_t st);
 
 // Which kernel a windowed Default call with many rows takes.  Where 128-row items
-// all run at once (two to a CU at D = 64), the latency of a step sets the time, and
-// the kernel of attn_fwd.hpp with 128-key blocks wins, whose keys are split over
-// two waves (GQA 32/8, D = 128: 512 positions, window 256, 13.2 us against the tile
-// kernel's 16.2; 900, 1700: 40 against 65; 16 heads of 600 at D = 64, 300: 13.4
-// against 16.4; of 2300, 4000: 83 against 113).  With items for a third of the CUs
-// only and more than 1536 keys, the tile kernel's workgroups split the keys (100
-// positions, window 4096: 58 -> 31 us; 300, 2000: 40 -> 41; with items for half of
-// the CUs, 16 heads of 1000 at D = 64, 2000, it would be 26 -> 40, the parts' join
-// being most of it).  With more items the products bind, and the tile kernel wins
-// (16384 positions, window 4096: 1020 -> 973 us; D = 64, 32 heads of 2300, 4000:
-// 152 -> 133).
+// all run at once, one to a CU, the latency of a step sets the time, and the kernel
+// of attn_fwd.hpp with 128-key blocks wins, whose keys are split over two waves (GQA
+// 32/8, D = 128: 512 positions, window 256, 13.9 us against the tile kernel's 16.6;
+// 900, 1700: 41 against 50; 16 heads of 600 at D = 64, 300: 13.9 against 15.5).  With
+// items for a third of the CUs only and more than 1536 keys, the tile kernel's
+// workgroups split the keys (100 positions, window 4096: 58 -> 29 us, 100 whole; with
+// items for half of the CUs, 16 heads of 1000 at D = 64, 2000, it would be 27 -> 30,
+// the parts' join being most of it).  With more items the products bind, and the
+// tile kernel wins (16384 positions, window 4096: 1020 -> 973 us; D = 64, 16 heads
+// of 2300, 4000: 89 -> 84).
 struct WindowForm {
     int rows;                       // of a workgroup: 64 or 128 (two waves on the same rows) ..
     bool tile;                      // .. or, of the tile kernel, 128 or 256
@@ -315,8 +314,7 @@ inline WindowForm window_form(int D, long long flat, int group, long long heads,
     const long long n64 = (flat + 63) / 64 * heads, n128 = (flat + 127) / 128 * heads;
     const long long reach = window + sinks + 128 / group + 1, keys = reach < Sk ? reach : Sk;
     if (3 * n128 <= ncu && keys > 1536) return {128, true, keys};
-    if (n64 <= ncu || (D == 64 && n128 <= 2 * ncu)) return {64, false, 0};
-    if (D == 128 && n128 <= ncu) return {128, false, 0};
+    if (n128 <= ncu) return {D == 64 || n64 <= ncu ? 64 : 128, false, 0};
     return {D == 64 ? 128 : 256, true, 0};
 }
 

@@ -99,7 +99,7 @@ def test_default_split_keys_many_rows(shape):
     _default(shape, 1700, 70, 64)
 
 
-@pytest.mark.parametrize("shape", [(1, 16, 16, 1100, 1100, 64), (4, 35, 35, 400, 401, 64), (1, 32, 8, 1100, 1100, 128),
+@pytest.mark.parametrize("shape", [(1, 16, 16, 1100, 1100, 64), (4, 35, 35, 400, 401, 64), (2, 20, 20, 1000, 1003, 64), (1, 32, 8, 1100, 1100, 128),
                                    (3, 20, 4, 600, 601, 128), (1, 32, 8, 1500, 1200, 128), (1, 8, 8, 2100, 2100, 128)])
 def test_default_many_items(shape):
     """More workgroups than CUs, or than 64- or 128-row items would be: the tile kernel, and the forms beside it."""
