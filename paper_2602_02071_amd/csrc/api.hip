@@ -776,10 +776,17 @@ int baps_cache_attention(const baps_cache_t* cache, int layer, const void* q, lo
         p.scale = scale_log2 > 0.0f ? scale_log2 : (float)(1.4426950408889634 / std::sqrt((double)cache->D));
         // K and V that one call streams past the 256 MiB cache in front of memory
         // are read without leaving them there, when one workgroup reads them (64
-        // sequences of 5000 to 8192 keys, 436 MB: 160 -> 150 us; where they
+        // sequences of 5000 to 8192 keys, 872 MB: 160 -> 150 us; where they
         // fit and are read again soon it loses: 157 MB at D = 64, 39 -> 41)
         const long long reach = window > 0 && (long long)window + sinks + max_q < max_len ? (long long)window + sinks + max_q : max_len;
         p.once = 2LL * B * reach * cache->Hkv * cache->D > (256LL << 20);
+        int ncu = 0;
+        const hipError_t e = cu_count(&ncu);
+        if (e != hipSuccess) return status_of(e);
+        const long long groups = (long long)cache->Hkv * p.nsplit;    // workgroups of a sequence
+        // (the order costs 2 us: 64 sequences of 500 keys 15.7 -> 17.9)
+        const bool longish = reach >= 1024LL * p.nsplit;
+        p.chunk = longish && B <= 64 && B * groups > ncu && groups <= ncu ? (int)(ncu / groups) : 0;
         p.part = static_cast<float*>(workspace);
         p.ml = p.part + (long long)p.nsplit * total_q * Hq * cache->D;
         clear_stale_error();

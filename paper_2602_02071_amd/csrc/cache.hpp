@@ -43,6 +43,7 @@ struct CacheAttnParams {
     int window, sinks;              // window 0: none
     float scale;                    // score scale in log2 units
     bool once;                      // the cache is read once and does not stay in the caches on the way
+    int chunk;                      // > 0: places of sequence_of_place (cache_attention.hip)
     int nsplit;                     // > 1: partial results go to part / ml
     float* part;                    // [nsplit][total_q * Hq][D] unnormalised sums
     float* ml;                      // [nsplit][total_q * Hq][2] running maximum (log2 units) and sum

@@ -85,10 +85,27 @@ __device__ __forceinline__ uint32_t byte_mask(uint32_t seen, int w)
 // the way: the loads of step j+1 go out as soon as the registers of step j are
 // read.  P enters P V as two bf16 terms (P = hi + lo to 2^-17): the second
 // product is free where the bytes bound the kernel (64 sequences of 5000 to 8192
-// keys, GQA 32/8, D = 128: 151 us, 5.8 TB/s).
+// keys, GQA 32/8, D = 128: 140 us, 6.2 TB/s).
 constexpr int kStep = 64;
 constexpr int kRows = 16;
 constexpr int kWaves = 4;
+
+// The sequence of place z in the order longest first, every other `chunk` places in
+// reverse: the workgroups of one chunk take a CU each, so that a CU's two hold a long
+// and a short sequence, and none is done long before the others (64 sequences, GQA
+// 32/8, D = 128, of 5000 to 8192 keys: 150 -> 140 us; of 1000 to 9000: 142 -> 111; of
+// one length: 136 -> 139).  One lane per sequence; B <= 64.
+__device__ __forceinline__ int sequence_of_place(const CacheAttnParams& p, int z, int chunk, int lane)
+{
+    // (different for all, so that every place has one)
+    const uint32_t key = lane < p.B ? (uint32_t)min(max(p.lens[lane], 0), (1 << 26) - 1) << 6 | (63 - lane) : 0;
+    int rank = 0;
+#pragma unroll 4
+    for (int j = 0; j < p.B; ++j) rank += (uint32_t)__builtin_amdgcn_readlane(key, j) > key ? 1 : 0;
+    const int first = z / chunk * chunk, last = min(first + chunk, p.B) - 1;
+    const int want = (z / chunk) & 1 ? first + last - z : z;
+    return __builtin_ctzll(__ballot(lane < p.B && rank == want));
+}
 
 template <int D, int TR, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAttnParams p)
@@ -105,7 +122,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void baps_cache_rows_kernel(CacheAt
     const int G = p.Hq / p.c.Hkv;
     const int split = blockIdx.x;
     const int h = blockIdx.y % p.c.Hkv, tile = blockIdx.y / p.c.Hkv;
-    const int b = blockIdx.z;
+    int b = blockIdx.z;
+    if (p.chunk > 0) b = sequence_of_place(p, b, p.chunk, lane);
     const Seq s = sequence(p, b);
     const int f0 = tile * kTile, flat = s.n * G;
     if (f0 >= flat) return;
@@ -848,6 +866,18 @@ double tile_time(int n, int D, double blocks, double avg, double groups, double 
     return step * (longest > shared ? longest : shared) + (n > 1 ? 6.0 + rows * n * 8 * D / 5e6 : 0.0);
 }
 
+// The same of the rows kernel where its workgroups are more than the CUs: a CU takes
+// 25 GB/s of codes, whether one or two workgroups read them, so the one with most
+// sets the time (40 sequences of 6600 keys, 320 workgroups: 120 us, 102, 95 and 94
+// with two, three and four splits; 64 of them, 512 workgroups: 141, 144, 145, 148.
+// At D = 64, where more workgroups share a CU, 400 of them take 62 whole, 77, 64 and
+// 72.)
+double rows_time(int n, int D, double keys, long long groups, double rows, int ncu)
+{
+    const long long of_a_cu = (groups * n + ncu - 1) / ncu;
+    return of_a_cu * keys / n * 2 * D / 25e3 * (1 + 0.02 * (n - 1)) + (n > 1 ? 4.0 + rows * n * 8 * D / 5e6 : 0.0);
+}
+
 int cache_attention_splits(int B, int Hq, int Hkv, int D, int total_q, int max_q, int max_len, int window, int sinks, int ncu)
 {
     const long long flat = (long long)max_q * (Hq / Hkv);
@@ -860,8 +890,18 @@ int cache_attention_splits(int B, int Hq, int Hkv, int D, int total_q, int max_q
     if (window > 0 && span < keys) keys = span;
     const long long blocks = (keys + kStep - 1) / kStep;
     if (few) {
-        const long long n = std::min(2LL * ncu / groups, blocks / (2 * kWaves));    // two waves' blocks per split at least
-        return (int)std::min(std::max(n, 1LL), (long long)kMaxSplits);
+        const int most = (int)std::min(blocks / (2 * kWaves), (long long)kMaxSplits);   // two steps per wave and split at least
+        if (groups <= ncu) return std::max(std::min((int)(2 * ncu / groups), most), 1);
+        int best = 1;
+        double least = 0.9 * rows_time(1, D, keys, groups, 0, ncu);
+        for (int n = 2; D == 128 && n <= std::min(most, kFewSplits); ++n) {
+            const double t = rows_time(n, D, keys, groups, (double)total_q * Hq, ncu);
+            if (t < least) {
+                least = t;
+                best = n;
+            }
+        }
+        return best;
     }
     const double avg = window > 0 ? (double)blocks : std::max((double)blocks - max_q / 128.0, blocks / 2.0);
     const double whole = tile_time(1, D, blocks, avg, groups, (double)total_q * Hq, ncu);

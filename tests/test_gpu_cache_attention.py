@@ -219,6 +219,16 @@ def test_many_sequences(B):
     _run(29, lens, new, 4, 2, 128, 16, 20, 3)
 
 
+@pytest.mark.parametrize("B,D,window", [(40, 128, 0), (64, 64, 0), (33, 128, 1200), (63, 128, 0)])
+def test_large_ragged_decode(B, D, window):
+    """More workgroups than CUs: sequences taken in another order than the batch's, keys split or not."""
+    lens = [(211 * b) % 700 + 1 for b in range(B)]
+    lens[5], lens[6], lens[B - 1], lens[7], lens[8] = 2300, 0, 2300, 640, 640
+    new = [min(n, 1) for n in lens]
+    _run(31, lens, new, 8, 8, D, 64, window, 5 if window else 0)
+    _run(32, lens, [min(n, 1 + b % 3) for b, n in enumerate(lens)], 16, 8, D, 64, window, 0, max_len=5000)
+
+
 def test_strided_rows_and_scale():
     """q as a slice of a wider projection; a score scale of the caller's."""
     pool = H.Pool(22, 1, 12, 2, 32, 128)
