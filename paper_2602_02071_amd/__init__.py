@@ -502,6 +502,14 @@ class PagedCache:
         self._call(run)
         return o, l
 
+    def _int_outputs(self, nbytes, *sizes, stream):
+        """A workspace of nbytes and int32 outputs, parts of one allocation (one costs the host as much as a small kernel)."""
+        ws, *outs = self.k_exp.new_empty(nbytes // 4 + sum(sizes), dtype=self._int32).split_with_sizes((nbytes // 4, *sizes))
+        if stream is not None:
+            import torch
+            ws.record_stream(torch.cuda.ExternalStream(_stream(stream), device=self.device))
+        return ws, *outs
+
     def fork(self, table, lens, refs, parent, grow=None, stream=None):
         """The next set of sequences: (table, lens, refs, missing), new tensors; the pool's copies are made in place."""
         B_in, B_out = lens.shape[0], parent.shape[0]
@@ -512,24 +520,18 @@ class PagedCache:
         if grow is not None:
             self._ints("grow", grow, 1, B_out)
         width = table.shape[1]
-        out, lens_out, refs_out, missing = (refs.new_empty(n) for n in ((B_out, width), B_out, self.num_pages, 1))
-
-        def run(c):
-            nbytes = baps_cache_pages_workspace(0, B_out)
-            baps_cache_fork(c, table, lens, refs, B_in, parent, grow, B_out, width, out, lens_out, refs_out, missing,
-                            _scratch(nbytes, self.device, stream), nbytes, stream)
-        self._call(run)
-        return out, lens_out, refs_out, missing
+        nbytes = baps_cache_pages_workspace(0, B_out)
+        ws, out, lens_out, refs_out, missing = self._int_outputs(nbytes, B_out * width, B_out, self.num_pages, 1, stream=stream)
+        self._call(baps_cache_fork, table, lens, refs, B_in, parent, grow, B_out, width, out, lens_out, refs_out, missing, ws,
+                   nbytes, stream)
+        return out.view(B_out, width), lens_out, refs_out, missing
 
     def compact(self, table, refs, stream=None):
         """(table, refs, remap, live), new tensors; the pool's pages are moved in place."""
         self._ints("table", table, 2)
         self._ints("refs", refs, 1, self.num_pages)
-        out, refs_out, remap, live = (refs.new_empty(n) for n in (table.shape, self.num_pages, self.num_pages, 1))
-
-        def run(c):
-            nbytes = baps_cache_pages_workspace(self.num_pages, 0)
-            baps_cache_compact(c, table, table.numel(), refs, out, refs_out, remap, live,
-                               _scratch(nbytes, self.device, stream), nbytes, stream)
-        self._call(run)
-        return out, refs_out, remap, live
+        n = self.num_pages
+        nbytes = baps_cache_pages_workspace(n, 0)
+        ws, out, refs_out, remap, live = self._int_outputs(nbytes, table.numel(), n, n, 1, stream=stream)
+        self._call(baps_cache_compact, table, table.numel(), refs, out, refs_out, remap, live, ws, nbytes, stream)
+        return out.view(table.shape), refs_out, remap, live
