@@ -301,7 +301,11 @@ hipError_t launch_window_combine(const AttnParams& p, int D, hipStream_t st);
 // items for half of the CUs, 16 heads of 1000 at D = 64, 2000, it would be 27 -> 30,
 // the parts' join being most of it).  With more items the products bind, and the
 // tile kernel wins (16384 positions, window 4096: 1020 -> 973 us; D = 64, 16 heads
-// of 2300, 4000: 89 -> 84).
+// of 2300, 4000: 89 -> 84).  At D = 128, two workgroups of 128 rows on a CU fill each
+// other's starts and ends, one of 256 rows loads K and V half as often: up to 2048
+// keys the former (16384 positions, window 256: 189 -> 170 us; 4 x 32 heads of 2000:
+// 180 -> 174), then the latter (16384, 4096: 974 against 995; 4096, 4096: 147
+// against 154).
 struct WindowForm {
     int rows;                       // of a workgroup: 64 or 128 (two waves on the same rows) ..
     bool tile;                      // .. or, of the tile kernel, 128 or 256
@@ -315,7 +319,7 @@ inline WindowForm window_form(int D, long long flat, int group, long long heads,
     const long long reach = window + sinks + 128 / group + 1, keys = reach < Sk ? reach : Sk;
     if (3 * n128 <= ncu && keys > 1536) return {128, true, keys};
     if (n128 <= ncu) return {D == 64 || n64 <= ncu ? 64 : 128, false, 0};
-    return {D == 64 ? 128 : 256, true, 0};
+    return {D == 64 || keys <= 2048 ? 128 : 256, true, 0};
 }
 
 // rows per key/value head up to which a call takes the few-rows kernel

@@ -100,11 +100,16 @@ def test_default_split_keys_many_rows(shape):
 
 
 @pytest.mark.parametrize("shape", [(1, 16, 16, 1100, 1100, 64), (4, 35, 35, 400, 401, 64), (2, 20, 20, 1000, 1003, 64), (1, 32, 8, 1100, 1100, 128),
-                                   (3, 20, 4, 600, 601, 128), (1, 32, 8, 1500, 1200, 128), (1, 8, 8, 2100, 2100, 128)])
+                                   (3, 20, 4, 600, 601, 128), (1, 32, 8, 1500, 1200, 128), (1, 8, 8, 2100, 2100, 128), (1, 12, 3, 3100, 3103, 128)])
 def test_default_many_items(shape):
     """More workgroups than CUs, or than 64- or 128-row items would be: the tile kernel, and the forms beside it."""
     for window, sinks, block in ((100, 0, 64), (333, 5, 128), (1, 1, 32), (64, 65, 64)):
         _default(shape, window, sinks, block)
+
+
+def test_default_tile_of_256_rows():
+    """Long windows on more 128-row items than CUs."""
+    _default((1, 33, 3, 3201, 3300, 128), 2900, 4, 64, out_bf16=True)
 
 
 def test_default_large_scores_and_scale():
