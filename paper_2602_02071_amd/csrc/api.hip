@@ -770,7 +770,7 @@ int baps_cache_attention(const baps_cache_t* cache, int layer, const void* q, lo
         p.o = static_cast<uint16_t*>(o);
         p.lse = lse;
         p.cu = cu_q; p.lens = lens; p.table = table;
-        p.table_width = table_width; p.B = B; p.Hq = Hq; p.total_q = total_q; p.max_q = max_q;
+        p.table_width = table_width; p.B = B; p.Hq = Hq; p.total_q = total_q; p.max_q = max_q; p.max_len = max_len;
         p.window = window < (1 << 30) ? window : (1 << 30);        // (no position lies higher, and differences fit an int)
         p.sinks = sinks;
         p.scale = scale_log2 > 0.0f ? scale_log2 : (float)(1.4426950408889634 / std::sqrt((double)cache->D));

@@ -39,7 +39,7 @@ struct CacheAttnParams {
     uint16_t* o;                    // [total_q][Hq][D] bf16
     float* lse;                     // [total_q][Hq] or null
     const int *cu, *lens, *table;
-    int table_width, B, Hq, total_q, max_q;
+    int table_width, B, Hq, total_q, max_q, max_len;
     int window, sinks;              // window 0: none
     float scale;                    // score scale in log2 units
     bool once;                      // the cache is read once and does not stay in the caches on the way

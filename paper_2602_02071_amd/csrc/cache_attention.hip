@@ -9,7 +9,7 @@
 //
 // Two kernels.  rows: up to 16 flattened (query position, head of the group)
 // rows of a key/value head per workgroup, for decode; bound by the cache's
-// bytes.  tile: 256 rows per workgroup, for chunks of a prompt; bound by the
+// bytes.  tile: 128 or 256 rows per workgroup, for chunks of a prompt; bound by the
 // matrix unit and the exponentials.  Either splits the keys of a row over
 // workgroups where rows alone are too few, and combine joins the parts.
 #include <algorithm>
@@ -807,12 +807,36 @@ __global__ __launch_bounds__(256) void baps_cache_combine_few_kernel(CacheAttnPa
 // 32 per workgroup
 constexpr long long kFewRows = 64;
 int few_rows_tile(long long flat) { return flat <= kRows ? kRows : 2 * kRows; }
-// Waves of 32 rows in a workgroup of the tile kernel: eight at D = 128, whose
-// tiles' LDS a CU holds once (four, twice: 994 -> 1109 us for 2048 rows on 32768
-// keys, the codes are turned to bf16 twice as often); four at D = 64, two
-// workgroups per CU (156 -> 147 us for four sequences of 3000 to 4000 keys, 16
-// heads).
-template <int D> constexpr int kTileWaves = D == 128 ? 8 : 4;
+// Waves of 32 rows in a workgroup of the tile kernel.  Four, with two workgroups per
+// CU that fill each other's starts and ends (D = 64: 156 -> 147 us for four sequences
+// of 3000 to 4000 keys, 16 heads; D = 128: four of 256 new on 1024 keys 42 -> 36); but
+// at D = 128 eight past 1536 keys, for codes are turned to bf16 half as often (2048
+// new on 32768 keys 1109 -> 994, 512 on 9000 99 -> 91).
+int tile_waves(int D, int max_len, int window, int sinks)
+{
+    const long long reach = (long long)window + sinks;
+    return D == 64 || (window > 0 && reach < max_len ? reach : max_len) <= 1536 ? 4 : 8;
+}
+
+template <int D, int NW>
+hipError_t launch_tile(const CacheAttnParams& p, long long flat, hipStream_t st)
+{
+    static DeviceOnce attr_set;
+    const int bytes = TileCore<D, false>::kLds;
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (!attr_set.is_done(dev)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&baps_cache_tile_kernel<D, NW>),
+                                hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+        attr_set.mark(dev);
+    }
+    const long long tiles = (flat + 32 * NW - 1) / (32 * NW);
+    hipLaunchKernelGGL((baps_cache_tile_kernel<D, NW>), dim3((unsigned)(tiles * p.B * p.c.Hkv * p.nsplit)), dim3(64 * NW), bytes,
+                       st, p);
+    return hipGetLastError();
+}
 
 template <int D>
 hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
@@ -825,20 +849,12 @@ hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
         else if (p.once) hipLaunchKernelGGL((baps_cache_rows_kernel<D, 1, true>), grid, wg, 0, st, p);
         else hipLaunchKernelGGL((baps_cache_rows_kernel<D, 1, false>), grid, wg, 0, st, p);
     } else {
-        static DeviceOnce attr_set;
-        const int bytes = TileCore<D, false>::kLds;
-        int dev = 0;
-        hipError_t e = hipGetDevice(&dev);
+        hipError_t e = hipSuccess;
+        if constexpr (D == 128)
+            e = tile_waves(D, p.max_len, p.window, p.sinks) == 8 ? launch_tile<128, 8>(p, flat, st) : launch_tile<128, 4>(p, flat, st);
+        else
+            e = launch_tile<64, 4>(p, flat, st);
         if (e != hipSuccess) return e;
-        if (!attr_set.is_done(dev)) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(&baps_cache_tile_kernel<D, kTileWaves<D>>),
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-            if (e != hipSuccess) return e;
-            attr_set.mark(dev);
-        }
-        const long long tiles = (flat + 32 * kTileWaves<D> - 1) / (32 * kTileWaves<D>);
-        hipLaunchKernelGGL((baps_cache_tile_kernel<D, kTileWaves<D>>), dim3((unsigned)(tiles * p.B * p.c.Hkv * p.nsplit)),
-                           dim3(64 * kTileWaves<D>), bytes, st, p);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.nsplit == 1) return e;
@@ -859,9 +875,9 @@ hipError_t launch_d(const CacheAttnParams& p, hipStream_t st)
 // two splits, 22 with four, 20 with eight; 32 heads over 8 of 3800, 1850 new, D =
 // 128: 115 whole, 121 with two; 32 over 8 of 9000, 512 new, D = 64: 94 with two, 67
 // with four, 64 with six.)
-double tile_time(int n, int D, double blocks, double avg, double groups, double rows, int ncu)
+double tile_time(int n, int D, int waves, double blocks, double avg, double groups, double rows, int ncu)
 {
-    const double step = D == 128 ? 2.0 : 1.4, at_once = D == 128 ? ncu : 2.0 * ncu;
+    const double step = D == 128 ? 2.0 : 1.4, at_once = waves == 8 ? ncu : 2.0 * ncu;
     const double longest = blocks / n, shared = groups * avg / at_once;
     return step * (longest > shared ? longest : shared) + (n > 1 ? 6.0 + rows * n * 8 * D / 5e6 : 0.0);
 }
@@ -882,7 +898,7 @@ int cache_attention_splits(int B, int Hq, int Hkv, int D, int total_q, int max_q
 {
     const long long flat = (long long)max_q * (Hq / Hkv);
     const bool few = flat <= kFewRows;
-    const int rows = few ? few_rows_tile(flat) : 32 * (D == 128 ? kTileWaves<128> : kTileWaves<64>);
+    const int waves = tile_waves(D, max_len, window, sinks), rows = few ? few_rows_tile(flat) : 32 * waves;
     // (ragged chunks: no more tiles than all rows fill, and one more each)
     const long long groups = Hkv * std::min((flat + rows - 1) / rows * B, (long long)total_q * (Hq / Hkv) / rows + B);
     long long keys = max_len;                                   // that a workgroup's rows reach
@@ -904,11 +920,11 @@ int cache_attention_splits(int B, int Hq, int Hkv, int D, int total_q, int max_q
         return best;
     }
     const double avg = window > 0 ? (double)blocks : std::max((double)blocks - max_q / 128.0, blocks / 2.0);
-    const double whole = tile_time(1, D, blocks, avg, groups, (double)total_q * Hq, ncu);
+    const double whole = tile_time(1, D, waves, blocks, avg, groups, (double)total_q * Hq, ncu);
     int best = 1;
     double least = 0.9 * whole;                                 // (a split is to gain a tenth)
     for (int n = 2; n <= kMaxSplits && n <= blocks; ++n) {
-        const double t = tile_time(n, D, blocks, avg, groups, (double)total_q * Hq, ncu);
+        const double t = tile_time(n, D, waves, blocks, avg, groups, (double)total_q * Hq, ncu);
         if (t < least) {
             least = t;
             best = n;

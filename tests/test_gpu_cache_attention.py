@@ -82,6 +82,14 @@ def test_chunk(page, D, window, sinks):
     _run(11 + page, [300, 100, 65, 0, 7], [70, 100, 1, 0, 7], 4, 2, D, page, window, sinks)
 
 
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2000, 30)])
+def test_chunk_of_long_calls(page, window, sinks):
+    """The wider tile of calls that announce long keys, whatever their sequences have."""
+    _run(33, [300, 100, 65, 0, 7], [70, 100, 1, 0, 7], 4, 2, 128, page, window, sinks, max_len=9000)
+    _run(34, [2300, 513], [101, 513], 3, 1, 128, page, window, sinks)
+
+
 @pytest.mark.parametrize("G", [1, 3, 8])
 def test_chunk_heads(G):
     _run(13, [410, 90], [100, 90], 2 * G, 2, 128, 64)
